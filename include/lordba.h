@@ -40,13 +40,14 @@ enum {
     LORDBA_ERR_NULL = 1,      /* a required pointer is NULL                                   */
     LORDBA_ERR_DIM = 2,       /* T < 0, d_in < 1, d_out < 1, r < 1, r > LORDBA_MAX_RANK, or a
                                  size that does not fit 32-bit indexing of one row             */
-    LORDBA_ERR_VALUE = 3,     /* a sign entry that is not +-1 (int8 variant) or is NaN (f32)  */
+    LORDBA_ERR_VALUE = 3,     /* a sign entry that is not +-1 (int8 variant) or is NaN (f32); a parameter
+                                 outside its range (tau, mu, digits, p)                          */
     LORDBA_ERR_ALIAS = 4,     /* y_out overlaps an input other than being exactly y_base      */
     LORDBA_ERR_ALIGN = 5,     /* a pointer is not aligned to its element size                 */
     LORDBA_ERR_NO_DEVICE = 6, /* no usable HIP device / not a gfx950 device                   */
     LORDBA_ERR_LAUNCH = 7,    /* the HIP runtime rejected the launch                          */
     LORDBA_ERR_ALGO = 8,      /* lordba_forward_algo: the requested kernel cannot run this shape */
-    LORDBA_ERR_WORKSPACE = 9  /* lordba_backward, lordba_ptq: the workspace is smaller than their ..._workspace_bytes */
+    LORDBA_ERR_WORKSPACE = 9  /* the workspace is smaller than the call's ..._workspace_bytes    */
 };
 
 #define LORDBA_MAX_RANK 64
@@ -399,6 +400,87 @@ size_t lordba_ptq_workspace_bytes(int64_t N, int64_t M, int64_t R, int64_t r0);
  * Rank decision: a pivot of the diagonally pivoted Cholesky factorisation that does not exceed 64 eps max_k G_kk ends
  * the factorisation; G = 0 gives beta = 0. */
 lordba_status lordba_ptq_beta_solve(const double* G, const double* h, double* beta, int64_t R, void* stream);
+
+/* ---- what stands around the branch: 8-bit base projections, the gated block, dropout ------------------------------- */
+
+/* The frozen base projection of an adapter, y_base = x W^T, with W held in 8 bits: int8 entries and an fp32 scale per output channel (the
+ * real weight is W[j, i] * w_scale[j]).  The rows of the activations are brought to integers inside the call, the sums are exact 32-bit
+ * integers, and y is rounded once:
+ *     amax_t = max_i |x[t, i]|,  D = 127 (digits = 1) or 127 * 256 (digits = 2)
+ *     q[t, i] = rint(x[t, i] * (D / amax_t)),  s_t = amax_t / D         (fp32; ties to even; a row of zeros has s_t = 0)
+ *     y[t, j] = fp16(s_t * w_scale[j] * sum_i q[t, i] * W[j, i])
+ * digits = 1 holds a row in one int8 each, digits = 2 in two (q = 256 hi + lo, 16 bits): twice the multiplications, and a rounding of the
+ * rows below that of fp16.  A row that holds an infinity or a NaN gives NaN in all of its results, in other rows nothing.
+ * Laid-out matrices: int8 [rows, lordba_i8_row_bytes(cols)], row-major, zeros behind column cols.  lordba_layout_i8 brings plain int8
+ * matrices into that form once; lordba_quantize_rows makes it from fp16 (weights, or rows of activations). */
+#define LORDBA_I8_MAX_COLUMNS 131071   /* longest contraction whose sum stays inside 32 bits */
+
+/* Bytes from one row to the next of a laid-out int8 matrix (0 for cols outside 1 .. LORDBA_I8_MAX_COLUMNS). */
+size_t lordba_i8_row_bytes(int64_t cols);
+
+/* Bytes of workspace for T rows of `cols` numbers in 1 or 2 digits (0 for arguments out of range). */
+size_t lordba_i8_workspace_bytes(int64_t T, int64_t cols, int digits);
+
+/* DEVICE function: lays out the plain row-major int8 matrix w [rows, cols] as [rows, lordba_i8_row_bytes(cols)], or, transposed != 0, its
+ * transpose as [cols, lordba_i8_row_bytes(rows)] (what the input gradients take).  out: 16-byte aligned, no overlap with w. */
+lordba_status lordba_layout_i8(const int8_t* w, int8_t* out, int64_t rows, int64_t cols, int transposed, void* stream);
+
+/* DEVICE function: rows of fp16 numbers x [rows, cols] (contiguous; times col_scale[cols] where that is not NULL) as integers:
+ *   q     : int8 [rows, lordba_i8_row_bytes(cols)], for digits = 2 [2, rows, ...]: all hi, then all lo; 16-byte aligned
+ *   scale : fp32 [rows]
+ * by the definition above.  A row whose largest magnitude is below 2^-100 counts as zeros; one that is not finite has q = 0 and the
+ * scale NaN.  Outputs must not overlap inputs or each other (LORDBA_ERR_ALIAS); digits other than 1, 2 -> LORDBA_ERR_VALUE. */
+lordba_status lordba_quantize_rows(const void* x, const float* col_scale, int8_t* q, float* scale, int64_t rows, int64_t cols, int digits,
+                                   void* stream);
+
+/* DEVICE function: y = x W^T by the definition above.
+ *   x fp16 [T, d_in]; W laid-out int8 [d_out, .]; w_scale fp32 [d_out]; y fp16 [T, d_out] (out)
+ *   workspace: lordba_i8_workspace_bytes(T, d_in, digits) bytes, 16-byte aligned, contents irrelevant; smaller -> LORDBA_ERR_WORKSPACE.
+ *   Calls that share a workspace must not overlap in time.
+ * Any T >= 0 (0: no work), 1 <= d_in <= LORDBA_I8_MAX_COLUMNS, 1 <= d_out <= 2^24; activations aligned to their elements.  The call
+ * only enqueues kernels on `stream`; it never synchronises, allocates or frees.  No output nor the workspace may overlap an input or
+ * each other (LORDBA_ERR_ALIAS). */
+lordba_status lordba_linear_i8(const void* x, const int8_t* W, const float* w_scale, void* y, void* workspace, size_t workspace_bytes,
+                               int64_t T, int64_t d_in, int64_t d_out, int digits, void* stream);
+
+/* DEVICE function: the gradient of y = x W^T with respect to x, dx[t, i] = sum_j g[t, j] w_scale[j] W[j, i] (what lordba_backward takes as
+ * dx_base).  g fp16 [T, d_out]; Wt: the transposed layout of W, int8 [d_in, lordba_i8_row_bytes(d_out)]; w_scale fp32 [d_out]; dx fp16
+ * [T, d_in].  The rows g * w_scale are held in `digits` digits: with 2 the error per entry of a row is at most its largest entry / 65024.
+ * workspace: lordba_i8_workspace_bytes(T, d_out, digits).  1 <= d_out <= LORDBA_I8_MAX_COLUMNS; everything else as lordba_linear_i8. */
+lordba_status lordba_linear_i8_backward(const void* g, const int8_t* Wt, const float* w_scale, void* dx, void* workspace, size_t workspace_bytes,
+                                        int64_t T, int64_t d_in, int64_t d_out, int digits, void* stream);
+
+/* DEVICE function: the gated feed-forward block's first half in one product kernel,
+ *     gate = x Wg^T + addends[0],  up = x Wu^T + addends[1],  h = gate * sigma(gate) * up        (sigma: the logistic function)
+ *   x fp16 [T, d_in]; W laid-out int8 [2 d_ff, .], the rows of Wg, then those of Wu; w_scale fp32 [2 d_ff];
+ *   addends fp16 [2, T, d_ff] or NULL: what is added to the projections before the activation (the adapters' branches: lordba_forward with
+ *   y_base = 0); h fp16 [T, d_ff]; gate_up fp16 [2, T, d_ff] or NULL: gate and up, kept for the backward pass.
+ * gate and up enter h before they are rounded.  workspace: lordba_i8_workspace_bytes(T, d_in, digits).  Everything else as
+ * lordba_linear_i8; 1 <= d_ff <= 2^24. */
+lordba_status lordba_gated_i8(const void* x, const int8_t* W, const float* w_scale, const void* addends, void* h, void* gate_up,
+                              void* workspace, size_t workspace_bytes, int64_t T, int64_t d_in, int64_t d_ff, int digits, void* stream);
+
+/* DEVICE function: its backward pass.  From dh fp16 [T, d_ff] and the kept gate_up:
+ *     dgate = dh * up * sigma(gate) * (1 + gate * (1 - sigma(gate))),  dup = dh * gate * sigma(gate)
+ *     dx = dgate diag(w_scale) Wg + dup diag(w_scale) Wu
+ *   Wt: the transposed layout of the [2 d_ff, d_in] weights, int8 [d_in, lordba_i8_row_bytes(2 d_ff)]; dx fp16 [T, d_in];
+ *   dgate_up fp16 [2, T, d_ff]: dgate and dup, the upstream gradients of the two adapters (lordba_backward).
+ * dx takes dgate and dup before they are rounded to fp16, one token's 2 d_ff numbers as one row of `digits` digits.
+ * workspace: lordba_i8_workspace_bytes(T, 2 d_ff, digits).  2 d_ff <= LORDBA_I8_MAX_COLUMNS; everything else as lordba_linear_i8. */
+lordba_status lordba_gated_i8_backward(const void* dh, const void* gate_up, const int8_t* Wt, const float* w_scale, void* dx, void* dgate_up,
+                                       void* workspace, size_t workspace_bytes, int64_t T, int64_t d_in, int64_t d_ff, int digits, void* stream);
+
+/* DEVICE function: dropout, with a mask that is a function of the element's index and never stored:
+ *     y_out[i] = y_base[i] + (draw(i) >= L ? x[i] * 65536 / (65536 - L) : 0),   L = rint(65536 p),  i < n
+ * draw(i): Philox4x32-10 with the 128-bit counter (i / 8, offset + *offset_dev), 64 bits each, low word first, and the key `seed`; element
+ * e = i mod 8 takes 16 bits, word e / 2 shifted right by 16 (e mod 2).  The kept share is exactly (65536 - L) / 65536, and x is divided by
+ * that.  p = 0 keeps everything, p = 1 nothing.  What is dropped contributes 0 whatever it is.
+ * The backward pass is the same call on the gradient with the same seed and offset, with the base path's gradient as y_base.
+ *   x, y_out fp16 [n]; y_base fp16 [n] or NULL (0); y_out may be x or y_base itself, any other overlap -> LORDBA_ERR_ALIAS.
+ *   offset_dev: one uint64 in device memory or NULL (0): a program that replays a captured graph moves the mask by writing it.
+ * p outside [0, 1] or NaN -> LORDBA_ERR_VALUE.  n <= 2^38.  Enqueues one kernel; never synchronises, allocates or frees. */
+lordba_status lordba_dropout(const void* x, const void* y_base, void* y_out, int64_t n, double p, uint64_t seed, uint64_t offset,
+                             const uint64_t* offset_dev, void* stream);
 
 /* Static, never-NULL description of a status code. */
 const char* lordba_status_string(lordba_status status);

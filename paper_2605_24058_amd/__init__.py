@@ -6,7 +6,9 @@ binding functions load ``liblordba.so`` on first use and raise if it is missing.
 from . import inputs  # noqa: F401
 
 __all__ = ["inputs", "lordba_pack_signs", "lordba_forward", "lordba_packed_words",
-           "lordba_status_string", "load_library", "build_library"]
+           "lordba_status_string", "load_library", "build_library",
+           "lordba_i8_row_bytes", "lordba_i8_workspace_bytes", "lordba_layout_i8", "lordba_quantize_rows", "lordba_linear_i8",
+           "lordba_linear_i8_backward", "lordba_gated_i8", "lordba_gated_i8_backward", "lordba_dropout"]
 
 
 def __getattr__(name):

@@ -7,6 +7,7 @@ the current torch stream is passed as the hipStream_t.
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes
 import importlib
 import os
@@ -25,7 +26,8 @@ _LIB_PATH = os.path.join(_PKG, "liblordba.so")
 # one translation unit per kernel family and kind (inference / training): they compile side by side
 _SOURCES = ("lordba_forward.hip", "lordba_forward_train.hip", "lordba_forward_any.hip", "lordba_forward_any_train.hip",
             "lordba_forward_multi_l2.hip", "lordba_forward_multi_l3.hip", "lordba_forward_multi_l4.hip",
-            "lordba_forward_multi_train.hip", "lordba_forward_multi.hip", "lordba_backward.hip", "lordba_ptq.hip", "lordba_pack_device.hip", "lordba_pack.cpp")
+            "lordba_forward_multi_train.hip", "lordba_forward_multi.hip", "lordba_backward.hip", "lordba_ptq.hip", "lordba_pack_device.hip", "lordba_pack.cpp",
+            "lordba_i8_rows.hip", "lordba_i8_product.hip", "lordba_dropout.hip")
 _lib = None
 _TORCH_MODULE_PATH = os.path.join(_PKG, "_lordba_torch.so")
 _torch_module = None
@@ -218,6 +220,24 @@ def load_library():
     lib.lordba_ptq_sweeps.argtypes = [vp] * 12 + [ctypes.c_size_t] + [i64] * 7 + [ctypes.c_double, ctypes.c_double, vp]
     lib.lordba_ptq_beta_solve.restype = ci
     lib.lordba_ptq_beta_solve.argtypes = [vp, vp, vp, i64, vp]
+    lib.lordba_i8_row_bytes.restype = ctypes.c_size_t
+    lib.lordba_i8_row_bytes.argtypes = [i64]
+    lib.lordba_i8_workspace_bytes.restype = ctypes.c_size_t
+    lib.lordba_i8_workspace_bytes.argtypes = [i64, i64, ci]
+    lib.lordba_layout_i8.restype = ci
+    lib.lordba_layout_i8.argtypes = [vp, vp, i64, i64, ci, vp]
+    lib.lordba_quantize_rows.restype = ci
+    lib.lordba_quantize_rows.argtypes = [vp] * 4 + [i64, i64, ci, vp]
+    for name in ("lordba_linear_i8", "lordba_linear_i8_backward"):
+        f = getattr(lib, name)
+        f.restype = ci
+        f.argtypes = [vp] * 5 + [ctypes.c_size_t] + [i64] * 3 + [ci, vp]
+    for name in ("lordba_gated_i8", "lordba_gated_i8_backward"):
+        f = getattr(lib, name)
+        f.restype = ci
+        f.argtypes = [vp] * 7 + [ctypes.c_size_t] + [i64] * 3 + [ci, vp]
+    lib.lordba_dropout.restype = ci
+    lib.lordba_dropout.argtypes = [vp] * 3 + [i64, ctypes.c_double, ctypes.c_uint64, ctypes.c_uint64, vp, vp]
     lib.lordba_status_string.restype = ctypes.c_char_p
     lib.lordba_status_string.argtypes = [ci]
     _lib = lib
@@ -808,3 +828,232 @@ def to_device(inputs: dict, device="cuda:0") -> dict:
     dev["packedA"] = torch.from_numpy(pA.view(np.int32)).to(device)
     dev["packedB"] = torch.from_numpy(pB.view(np.int32)).to(device)
     return dev
+
+
+# ---- what stands around the branch: 8-bit base projections, the gated block, dropout ----
+
+I8_MAX_COLUMNS = 131071
+
+
+def lordba_i8_row_bytes(cols: int) -> int:
+    """Bytes from one row to the next of a laid-out int8 matrix with this many columns."""
+    return int(load_library().lordba_i8_row_bytes(cols))
+
+
+def lordba_i8_workspace_bytes(T: int, cols: int, digits: int = 1) -> int:
+    """Bytes of workspace for T rows of `cols` numbers: d_in of the forward calls, d_out (2 d_ff) of the backward calls."""
+    return int(load_library().lordba_i8_workspace_bytes(T, cols, digits))
+
+
+def _on_stream(stream):
+    """Where a call makes its outputs and its workspace: on the stream that its kernels run on, whose order then guards the memory."""
+    import torch
+
+    if stream is None:
+        return contextlib.nullcontext()
+    return torch.cuda.stream(stream if hasattr(stream, "cuda_stream") else torch.cuda.ExternalStream(stream))
+
+
+def _laid_out(w, rows, cols, what: str) -> None:
+    if tuple(w.shape) != (rows, lordba_i8_row_bytes(cols)):
+        raise ValueError("%s must be the layout of an int8 matrix [%d, %d] (lordba_layout_i8)" % (what, rows, cols))
+
+
+def _output(given, shape, like, what: str):
+    import torch
+
+    if given is None:
+        return torch.empty(shape, dtype=torch.float16, device=like.device)
+    _need(torch.float16, "float16 CUDA tensor", (what,), given)
+    if tuple(given.shape) != tuple(shape):
+        raise ValueError("%s must be %s" % (what, list(shape)))
+    return given
+
+
+def _i8_workspace(given, T, cols, digits, like):
+    import torch
+
+    if digits not in (1, 2):
+        raise ValueError("digits must be 1 or 2")
+    if given is None:
+        return torch.empty(max(lordba_i8_workspace_bytes(T, cols, digits), 16), dtype=torch.uint8, device=like.device)
+    if not given.is_cuda or not given.is_contiguous():
+        raise TypeError("workspace must be a contiguous CUDA tensor")
+    return given
+
+
+def lordba_layout_i8(w, transposed: bool = False, stream=None):
+    """Lays out a plain int8 matrix [rows, cols] (contiguous CUDA tensor) for the projections, once: int8
+    [rows, lordba_i8_row_bytes(cols)]; transposed: [cols, lordba_i8_row_bytes(rows)], which the input gradients take."""
+    import torch
+
+    lib = load_library()
+    _need(torch.int8, "int8 CUDA tensor", ("w",), w)
+    if w.dim() != 2:
+        raise ValueError("w must be [rows, cols]")
+    rows, cols = w.shape
+    n, k = (cols, rows) if transposed else (rows, cols)
+    with _on_stream(stream):
+        out = torch.empty((n, lordba_i8_row_bytes(k)), dtype=torch.int8, device=w.device)
+    st = lib.lordba_layout_i8(w.data_ptr(), out.data_ptr(), rows, cols, int(bool(transposed)), _stream_handle(w, stream))
+    if st != 0:
+        raise LordbaError(st, "lordba_layout_i8")
+    return out
+
+
+def lordba_quantize_rows(x, col_scale=None, digits: int = 1, stream=None):
+    """Rows of fp16 numbers x [rows, cols] (times the fp32 col_scale [cols]) as integers: (q, scale) with q int8
+    [rows, lordba_i8_row_bytes(cols)], for digits = 2 [2, rows, ...] with x ~ (256 q[0] + q[1]) scale; scale fp32 [rows]."""
+    import torch
+
+    lib = load_library()
+    _need(torch.float16, "float16 CUDA tensor", ("x",), x)
+    if x.dim() != 2:
+        raise ValueError("x must be [rows, cols]")
+    rows, cols = x.shape
+    if col_scale is not None:
+        _need(torch.float32, "float32 CUDA tensor", ("col_scale",), col_scale)
+        if col_scale.numel() != cols:
+            raise ValueError("col_scale must be [cols]")
+    if digits not in (1, 2):
+        raise ValueError("digits must be 1 or 2")
+    ld = lordba_i8_row_bytes(cols)
+    with _on_stream(stream):
+        q = torch.empty((rows, ld) if digits == 1 else (2, rows, ld), dtype=torch.int8, device=x.device)
+        scale = torch.empty(rows, dtype=torch.float32, device=x.device)
+    st = lib.lordba_quantize_rows(x.data_ptr(), None if col_scale is None else col_scale.data_ptr(), q.data_ptr(), scale.data_ptr(),
+                                  rows, cols, digits, _stream_handle(x, stream))
+    if st != 0:
+        raise LordbaError(st, "lordba_quantize_rows")
+    return q, scale
+
+
+def lordba_linear_i8(x, W, w_scale, digits: int = 1, y_out=None, workspace=None, stream=None):
+    """The frozen base projection y = x W^T on 8-bit weights: x fp16 [T, d_in], W the layout of int8 [d_out, d_in], w_scale fp32
+    [d_out]; the rows of x in one digit (8 bits) or two (16).  Returns y fp16 [T, d_out], what lordba_forward takes as y_base."""
+    import torch
+
+    lib = load_library()
+    _need(torch.float16, "float16 CUDA tensor", ("x",), x)
+    _need(torch.int8, "int8 CUDA tensor", ("W",), W)
+    _need(torch.float32, "float32 CUDA tensor", ("w_scale",), w_scale)
+    if x.dim() != 2:
+        raise ValueError("x must be [T, d_in]")
+    T, d_in = x.shape
+    d_out = w_scale.numel()
+    _laid_out(W, d_out, d_in, "W")
+    with _on_stream(stream):
+        y_out = _output(y_out, (T, d_out), x, "y_out")
+        ws = _i8_workspace(workspace, T, d_in, digits, x)
+    st = lib.lordba_linear_i8(x.data_ptr(), W.data_ptr(), w_scale.data_ptr(), y_out.data_ptr(), ws.data_ptr(), ws.numel() * ws.element_size(),
+                              T, d_in, d_out, digits, _stream_handle(x, stream))
+    if st != 0:
+        raise LordbaError(st, "lordba_linear_i8")
+    return y_out
+
+
+def lordba_linear_i8_backward(g, Wt, w_scale, digits: int = 2, dx_out=None, workspace=None, stream=None):
+    """The gradient of that projection with respect to x: g fp16 [T, d_out], Wt the transposed layout of W, w_scale fp32 [d_out];
+    g * w_scale in two digits unless asked otherwise.  Returns dx fp16 [T, d_in], what lordba_backward takes as dx_base."""
+    import torch
+
+    lib = load_library()
+    _need(torch.float16, "float16 CUDA tensor", ("g",), g)
+    _need(torch.int8, "int8 CUDA tensor", ("Wt",), Wt)
+    _need(torch.float32, "float32 CUDA tensor", ("w_scale",), w_scale)
+    if g.dim() != 2 or Wt.dim() != 2 or w_scale.numel() != g.shape[1]:
+        raise ValueError("g must be [T, d_out], Wt a layout [d_in, .], w_scale [d_out]")
+    T, d_out = g.shape
+    d_in = Wt.shape[0]
+    _laid_out(Wt, d_in, d_out, "Wt")
+    with _on_stream(stream):
+        dx_out = _output(dx_out, (T, d_in), g, "dx_out")
+        ws = _i8_workspace(workspace, T, d_out, digits, g)
+    st = lib.lordba_linear_i8_backward(g.data_ptr(), Wt.data_ptr(), w_scale.data_ptr(), dx_out.data_ptr(), ws.data_ptr(),
+                                       ws.numel() * ws.element_size(), T, d_in, d_out, digits, _stream_handle(g, stream))
+    if st != 0:
+        raise LordbaError(st, "lordba_linear_i8_backward")
+    return dx_out
+
+
+def lordba_gated_i8(x, W, w_scale, addends=None, digits: int = 1, save: bool = False, workspace=None, stream=None):
+    """h = silu(x Wg^T + addends[0]) * (x Wu^T + addends[1]) on 8-bit weights: x fp16 [T, d_in]; W the layout of int8 [2 d_ff, d_in],
+    gate's rows first; w_scale fp32 [2 d_ff]; addends fp16 [2, T, d_ff]: the branches of the two projections' adapters.
+    Returns h fp16 [T, d_ff]; save: (h, gate_up) with gate_up fp16 [2, T, d_ff] for lordba_gated_i8_backward."""
+    import torch
+
+    lib = load_library()
+    _need(torch.float16, "float16 CUDA tensor", ("x",), x)
+    _need(torch.int8, "int8 CUDA tensor", ("W",), W)
+    _need(torch.float32, "float32 CUDA tensor", ("w_scale",), w_scale)
+    if x.dim() != 2 or w_scale.numel() % 2:
+        raise ValueError("x must be [T, d_in], w_scale [2 d_ff]")
+    T, d_in = x.shape
+    d_ff = w_scale.numel() // 2
+    _laid_out(W, 2 * d_ff, d_in, "W")
+    if addends is not None:
+        _need(torch.float16, "float16 CUDA tensor", ("addends",), addends)
+        if tuple(addends.shape) != (2, T, d_ff):
+            raise ValueError("addends must be [2, T, d_ff]")
+    with _on_stream(stream):
+        h = _output(None, (T, d_ff), x, "h")
+        gate_up = _output(None, (2, T, d_ff), x, "gate_up") if save else None
+        ws = _i8_workspace(workspace, T, d_in, digits, x)
+    ptr = lambda t_: None if t_ is None else t_.data_ptr()
+    st = lib.lordba_gated_i8(x.data_ptr(), W.data_ptr(), w_scale.data_ptr(), ptr(addends), h.data_ptr(), ptr(gate_up), ws.data_ptr(),
+                             ws.numel() * ws.element_size(), T, d_in, d_ff, digits, _stream_handle(x, stream))
+    if st != 0:
+        raise LordbaError(st, "lordba_gated_i8")
+    return (h, gate_up) if save else h
+
+
+def lordba_gated_i8_backward(dh, gate_up, Wt, w_scale, digits: int = 2, workspace=None, stream=None):
+    """Backward pass of lordba_gated_i8: dh fp16 [T, d_ff], the kept gate_up, Wt the transposed layout of the [2 d_ff, d_in] weights.
+    Returns (dx fp16 [T, d_in], dgate_up fp16 [2, T, d_ff]); dgate_up holds the upstream gradients of the two adapters."""
+    import torch
+
+    lib = load_library()
+    _need(torch.float16, "float16 CUDA tensor", ("dh", "gate_up"), dh, gate_up)
+    _need(torch.int8, "int8 CUDA tensor", ("Wt",), Wt)
+    _need(torch.float32, "float32 CUDA tensor", ("w_scale",), w_scale)
+    if dh.dim() != 2 or Wt.dim() != 2 or tuple(gate_up.shape) != (2,) + tuple(dh.shape) or w_scale.numel() != 2 * dh.shape[1]:
+        raise ValueError("dh must be [T, d_ff], gate_up [2, T, d_ff], Wt a layout [d_in, .], w_scale [2 d_ff]")
+    T, d_ff = dh.shape
+    d_in = Wt.shape[0]
+    _laid_out(Wt, d_in, 2 * d_ff, "Wt")
+    with _on_stream(stream):
+        dx, dgate_up = _output(None, (T, d_in), dh, "dx"), _output(None, (2, T, d_ff), dh, "dgate_up")
+        ws = _i8_workspace(workspace, T, 2 * d_ff, digits, dh)
+    st = lib.lordba_gated_i8_backward(dh.data_ptr(), gate_up.data_ptr(), Wt.data_ptr(), w_scale.data_ptr(), dx.data_ptr(), dgate_up.data_ptr(),
+                                      ws.data_ptr(), ws.numel() * ws.element_size(), T, d_in, d_ff, digits, _stream_handle(dh, stream))
+    if st != 0:
+        raise LordbaError(st, "lordba_gated_i8_backward")
+    return dx, dgate_up
+
+
+def lordba_dropout(x, p: float, seed: int, offset: int = 0, y_base=None, y_out=None, offset_dev=None, stream=None):
+    """y = y_base + dropout(x): elements are dropped at probability p (a multiple of 1/65536), the kept ones divided by the exact kept share;
+    the mask follows from (seed, offset + offset_dev) and the element's index.  The backward pass is the same call on the gradient.
+    x fp16 of any shape; y_base like x or None; offset_dev: int64 CUDA tensor of one element or None."""
+    import torch
+
+    lib = load_library()
+    _need(torch.float16, "float16 CUDA tensor", ("x",), x)
+    if y_base is not None:
+        _need(torch.float16, "float16 CUDA tensor", ("y_base",), y_base)
+        if y_base.shape != x.shape:
+            raise ValueError("y_base must have the shape of x")
+    if offset_dev is not None:
+        _need(torch.int64, "int64 CUDA tensor", ("offset_dev",), offset_dev)
+        if offset_dev.numel() != 1:
+            raise ValueError("offset_dev must hold one number")
+    if not 0 <= seed < 1 << 64 or not 0 <= offset < 1 << 64:
+        raise ValueError("seed and offset must be in [0, 2^64)")
+    with _on_stream(stream):
+        y_out = _output(y_out, tuple(x.shape), x, "y_out")
+    ptr = lambda t_: None if t_ is None else t_.data_ptr()
+    st = lib.lordba_dropout(x.data_ptr(), ptr(y_base), y_out.data_ptr(), x.numel(), float(p), seed, offset, ptr(offset_dev),
+                            _stream_handle(x, stream))
+    if st != 0:
+        raise LordbaError(st, "lordba_dropout")
+    return y_out

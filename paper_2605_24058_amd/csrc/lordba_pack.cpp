@@ -92,13 +92,13 @@ extern "C" const char* lordba_status_string(lordba_status status) {
         case LORDBA_OK: return "ok";
         case LORDBA_ERR_NULL: return "null pointer argument";
         case LORDBA_ERR_DIM: return "dimension out of range (need T >= 0, d_in, d_out >= 1, 1 <= r <= 64)";
-        case LORDBA_ERR_VALUE: return "carrier entry is not +1/-1 (or is NaN)";
+        case LORDBA_ERR_VALUE: return "value out of range: a carrier entry that is not +1/-1 (or is NaN), or a parameter";
         case LORDBA_ERR_ALIAS: return "y_out overlaps an input (only y_out == y_base is allowed)";
         case LORDBA_ERR_ALIGN: return "pointer not aligned to its element size";
         case LORDBA_ERR_NO_DEVICE: return "no usable gfx950 HIP device";
         case LORDBA_ERR_LAUNCH: return "HIP runtime rejected the kernel launch";
         case LORDBA_ERR_ALGO: return "requested kernel cannot run this shape or alignment";
-        case LORDBA_ERR_WORKSPACE: return "workspace smaller than lordba_backward_workspace_bytes";
+        case LORDBA_ERR_WORKSPACE: return "workspace smaller than the call's workspace_bytes";
         default: return "unknown status";
     }
 }
