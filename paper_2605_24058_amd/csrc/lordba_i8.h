@@ -18,7 +18,7 @@
 
 namespace {
 
-constexpr int64_t kI8Step = 128;   // columns that a row is padded to
+constexpr int64_t kI8Step = 256;   // columns that a row is padded to: up to four waves share a step of 64 each
 
 inline int64_t i8_row_bytes(int64_t cols) { return (cols + kI8Step - 1) / kI8Step * kI8Step; }
 

@@ -4,6 +4,8 @@
 // columns of y for one token.  Blocks of 16 rows are the unit of everything: with two digits the token blocks alternate hi, lo (y takes
 // 256 hi + lo of neighbouring accumulators), in the gated block the weight blocks alternate gate, up, so that a lane holds both
 // factors of its outputs.
+#include <algorithm>
+#include <cmath>
 #include <type_traits>
 
 #include "lordba_dev_util.h"
@@ -24,98 +26,105 @@ struct ProductArgs {
     int64_t T, n, ld;
 };
 
-typedef uint32_t u2_any __attribute__((ext_vector_type(2), aligned(2)));
 typedef float f4_any __attribute__((ext_vector_type(4), aligned(4)));
 
-// Four consecutive entries from column c of n: one access inside the row, single ones at its end.
-__device__ __forceinline__ void load4(const _Float16* row, int64_t c, int64_t n, float (&v)[4]) {
-    if (c + 4 <= n) {
-        const u2_any r = *reinterpret_cast<const u2_any*>(row + c);
-        const h2 a = as_h2(r[0]), b = as_h2(r[1]);
-        v[0] = a[0], v[1] = a[1], v[2] = b[0], v[3] = b[1];
+// Eight consecutive entries from column c of n; the part of a row that is there.
+template <bool FULL>
+__device__ __forceinline__ u4 load8(const _Float16* row, int64_t c, int64_t n) {
+    if (FULL || c + 8 <= n) return load16_any(row + c);
+    u4 v = {0u, 0u, 0u, 0u};
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+        if (c + e < n) v[e >> 1] |= static_cast<uint32_t>(reinterpret_cast<const uint16_t*>(row)[c + e]) << (16 * (e & 1));
+    return v;
+}
+template <bool FULL>
+__device__ __forceinline__ void load8(const float* p, int64_t c, int64_t n, float (&v)[8]) {
+    if (FULL || c + 8 <= n) {
+        const f4_any a = *reinterpret_cast<const f4_any*>(p + c), b = *reinterpret_cast<const f4_any*>(p + c + 4);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] = a[e], v[4 + e] = b[e];
     } else {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) v[i] = c + i < n ? static_cast<float>(row[c + i]) : 0.f;
+        for (int e = 0; e < 8; ++e) v[e] = c + e < n ? p[c + e] : 0.f;
     }
 }
-__device__ __forceinline__ void load4(const float* p, int64_t c, int64_t n, float (&v)[4]) {
-    if (c + 4 <= n) {
-        const f4_any r = *reinterpret_cast<const f4_any*>(p + c);
+template <bool FULL>
+__device__ __forceinline__ void store8(_Float16* row, int64_t c, int64_t n, const float (&f)[8]) {
+    h8 h;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) v[i] = r[i];
+    for (int e = 0; e < 8; ++e) h[e] = static_cast<_Float16>(f[e]);
+    const u4 v = __builtin_bit_cast(u4, h);
+    if (FULL || c + 8 <= n) {
+        *reinterpret_cast<u4_any*>(row + c) = v;
     } else {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) v[i] = c + i < n ? p[c + i] : 0.f;
-    }
-}
-__device__ __forceinline__ void store4(_Float16* row, int64_t c, int64_t n, const float (&v)[4]) {
-    if (c + 4 <= n) {
-        const h2 a = {static_cast<_Float16>(v[0]), static_cast<_Float16>(v[1])}, b = {static_cast<_Float16>(v[2]), static_cast<_Float16>(v[3])};
-        *reinterpret_cast<u2_any*>(row + c) = u2_any{__builtin_bit_cast(uint32_t, a), __builtin_bit_cast(uint32_t, b)};
-    } else {
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-            if (c + i < n) row[c + i] = static_cast<_Float16>(v[i]);
+        for (int e = 0; e < 8; ++e)
+            if (c + e < n) reinterpret_cast<uint16_t*>(row)[c + e] = static_cast<uint16_t>(v[e >> 1] >> (16 * (e & 1)));
     }
 }
 
-// The sums of a lane (CB x TB blocks) to y.  c0, t0: the first column of y and the first token of the wave's part.
-template <int CB, int TB, int DIG, bool GATED>
+// The sums of a lane (CB x TB blocks) to y.  c0, t0: the first column of y and the first token of the wave's part.  A lane has eight
+// consecutive columns of a token in a pair of weight blocks (of gate and of up each), see weight_row.  FULL: all columns and tokens exist.
+template <int CB, int TB, int DIG, bool GATED, bool FULL>
 __device__ __forceinline__ void finish(const ProductArgs& a, const i4 (&acc)[CB][TB], int64_t c0, int64_t t0) {
-    constexpr int P = GATED ? 2 : 1;
-    static_assert(CB % P == 0 && TB % DIG == 0, "whole pairs of blocks");
+    constexpr int P = GATED ? 2 : 1, G = 2 * P, J = TB / DIG;
+    static_assert(CB % G == 0 && TB % DIG == 0, "whole groups of blocks");
     const int lane = threadIdx.x & 63;
+    const int64_t plane = a.T * a.n, t1 = t0 + (lane & 15);
+    float s[J];
 #pragma unroll
-    for (int cb = 0; cb < CB; cb += P) {
-        const int64_t c = c0 + 16 * (cb / P) + 4 * (lane >> 4);
-        float w[P][4];
+    for (int j = 0; j < J; ++j) s[j] = FULL || t1 + 16 * j < a.T ? a.q_scale[t1 + 16 * j] : 0.f;
+#pragma unroll
+    for (int cb = 0; cb < CB; cb += G) {
+        const int64_t c = c0 + 32 * (cb / G) + 8 * (lane >> 4);
+        if (!FULL && c >= a.n) continue;
+        float w[P][8];
+        u4 add[P][J];
 #pragma unroll
         for (int p = 0; p < P; ++p) {
-            if (a.w_scale) load4(a.w_scale + p * a.n, c, a.n, w[p]);
-            else w[p][0] = w[p][1] = w[p][2] = w[p][3] = 1.f;
+            if (a.w_scale) load8<FULL>(a.w_scale + p * a.n, c, a.n, w[p]);
+            else w[p][0] = w[p][1] = w[p][2] = w[p][3] = w[p][4] = w[p][5] = w[p][6] = w[p][7] = 1.f;
+            if constexpr (GATED) {
+#pragma unroll
+                for (int j = 0; j < J; ++j)
+                    add[p][j] = a.addends && (FULL || t1 + 16 * j < a.T) ? load8<FULL>(a.addends + p * plane + (t1 + 16 * j) * a.n, c, a.n) : u4{0u, 0u, 0u, 0u};
+            }
         }
 #pragma unroll
-        for (int tb = 0; tb < TB; tb += DIG) {
-            const int64_t t = t0 + 16 * (tb / DIG) + (lane & 15);
-            if (t >= a.T || c >= a.n) continue;
-            const float s = a.q_scale[t];
-            float v[P][4];
+        for (int j = 0; j < J; ++j) {
+            const int64_t t = t1 + 16 * j;
+            if (!FULL && t >= a.T) continue;
+            float v[P][8];
 #pragma unroll
             for (int p = 0; p < P; ++p)
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    float sum = static_cast<float>(acc[cb + p][tb][i]);
-                    if constexpr (DIG == 2) sum = fmaf(256.f, sum, static_cast<float>(acc[cb + p][tb + 1][i]));
-                    v[p][i] = sum * s * w[p][i];
+                for (int e = 0; e < 8; ++e) {
+                    const int b = cb + (e >> 2) * P + p;
+                    float sum = static_cast<float>(acc[b][j * DIG][e & 3]);
+                    if constexpr (DIG == 2) sum = fmaf(256.f, sum, static_cast<float>(acc[b][j * DIG + 1][e & 3]));
+                    v[p][e] = sum * s[j] * w[p][e];
+                    if constexpr (GATED) v[p][e] += static_cast<float>(as_h8(add[p][j])[e]);
                 }
             if constexpr (GATED) {
-                const int64_t plane = a.T * a.n;
-                if (a.addends) {
-#pragma unroll
-                    for (int p = 0; p < 2; ++p) {
-                        float add[4];
-                        load4(a.addends + p * plane + t * a.n, c, a.n, add);
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) v[p][i] += add[i];
-                    }
-                }
                 if (a.kept) {
-                    store4(a.kept + t * a.n, c, a.n, v[0]);
-                    store4(a.kept + plane + t * a.n, c, a.n, v[1]);
+                    store8<FULL>(a.kept + t * a.n, c, a.n, v[0]);
+                    store8<FULL>(a.kept + plane + t * a.n, c, a.n, v[1]);
                 }
 #pragma unroll
-                for (int i = 0; i < 4; ++i) v[0][i] = v[0][i] / (1.f + __expf(-v[0][i])) * v[1][i];
+                for (int e = 0; e < 8; ++e) v[0][e] = v[0][e] / (1.f + __expf(-v[0][e])) * v[1][e];
             }
-            store4(a.y + t * a.n, c, a.n, v[0]);
+            store8<FULL>(a.y + t * a.n, c, a.n, v[0]);
         }
     }
 }
 
-// Row b * 16 + r of the workgroup's weight rows / token rows in memory.
+// Row b * 16 + r of the workgroup's weight rows / token rows in memory.  Two weight blocks (gated: two of gate and two of up in turn) hold
+// 32 columns such that rows 4 g .. 4 g + 3 of both are columns 8 g .. 8 g + 7: those that lane group g gets of the result.
 template <bool GATED>
 __device__ __forceinline__ const int8_t* weight_row(const ProductArgs& a, int64_t c0, int b, int r) {
-    if constexpr (GATED) return a.w + ((b & 1) * a.n + min(c0 + (b >> 1) * 16 + r, a.n - 1)) * a.ld;
-    else return a.w + min(c0 + b * 16 + r, a.n - 1) * a.ld;
+    const int group = GATED ? b >> 2 : b >> 1, half = GATED ? (b >> 1) & 1 : b & 1, up = GATED ? b & 1 : 0;
+    return a.w + (up * a.n + min(c0 + group * 32 + (r >> 2) * 8 + half * 4 + (r & 3), a.n - 1)) * a.ld;
 }
 template <int DIG>
 __device__ __forceinline__ const int8_t* token_row(const ProductArgs& a, int64_t t0, int b, int r) {
@@ -123,37 +132,56 @@ __device__ __forceinline__ const int8_t* token_row(const ProductArgs& a, int64_t
     else return a.q + min(t0 + b * 16 + r, a.T - 1) * a.ld;
 }
 
-// One workgroup: CT x TT sums (weight rows x token rows), WC x WT waves, steps of 64 columns through a ring of four slots in LDS.
+// Which tile a workgroup takes.  Workgroups go to the eight XCDs in turn, each with an L2 of its own: every XCD gets a contiguous eighth of the
+// tiles, in groups of kGroup tiles along the tokens, so that those it runs at a time share rows of both operands.
+constexpr uint32_t kGroup = 4;
+struct Tile {
+    uint32_t c, t;
+};
+__device__ __forceinline__ Tile tile_of(uint32_t id, uint32_t nc, uint32_t nt) {
+    const uint32_t n = nc * nt, xcd = id & 7, each = n / 8, rest = n % 8;
+    const uint32_t i = xcd * each + min(xcd, rest) + (id >> 3);
+    const uint32_t g = i / (kGroup * nc), in = i % (kGroup * nc), size = min(kGroup, nt - g * kGroup);
+    return {in / size, g * kGroup + in % size};
+}
+
+// One workgroup: CT x TT sums (weight rows x token rows) by WC x WT waves; with WK > 1 as many of those side by side, each with its own 64 columns of a
+// step (short steps wait for their barrier and for LDS, not for data: few tiles want long ones).  A ring of S slots in LDS holds the steps; the loads
+// go straight into it, several steps ahead.
 // A step's rows of 64 bytes lie there as four 16-byte pieces, piece p of row r at place p ^ (r / 2 mod 4): eight neighbouring
-// lanes of an operand read (eight rows, one piece) then cover all banks.  The loads go straight into LDS, where the place follows from
+// lanes of an operand read (eight rows, one piece) then cover all banks (no conflicts counted).  Where a load's data goes follows from
 // the lane, so it is the lane's address that is permuted.
 // While a step's products run on one set of operand registers, the next step's operands are read into the other.
-// The barrier of step k says that step k + 1 has landed and that everybody has read step k, whose slot then takes step k + 4.
-template <int CT, int TT, int WC, int WT, int DIG, bool GATED>
-__global__ __launch_bounds__(64 * WC * WT) void lordba_i8_product_kernel(ProductArgs a) {
-    constexpr int NW = WC * WT, CB = CT / 16 / WC, TB = TT / 16 / WT, NB = (CT + TT) / 16, L = NB / NW;
-    constexpr uint32_t kSlot = NB * 1024u;
-    static_assert(NB % NW == 0, "whole loads per wave");
+// The barrier of step k says that step k + 1 has landed and that everybody has read step k, whose slot then takes step k + S.
+template <int CT, int TT, int WC, int WT, int WK, int S, int DIG, bool GATED>
+__global__ __launch_bounds__(64 * WC * WT * WK) void lordba_i8_product_kernel(ProductArgs a) {
+    constexpr int NW = WC * WT * WK, CB = CT / 16 / WC, TB = TT / 16 / WT, NB = (CT + TT) / 16, L = NB * WK / NW;
+    constexpr uint32_t kPart = NB * 1024u, kSlot = WK * kPart;
+    static_assert(NB * WK % NW == 0 && (S == 3 || S == 4), "whole loads per wave; the waits at the end");
     extern __shared__ int8_t lds[];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int wc = wave % WC, wt = wave / WC;
+    const int wc = wave % WC, wt = wave / WC % WT, wk = wave / (WC * WT);
     constexpr int kCols = GATED ? CT / 2 : CT, kTokens = TT / DIG;
-    const int64_t c0 = static_cast<int64_t>(blockIdx.x) * kCols, t0 = static_cast<int64_t>(blockIdx.y) * kTokens;
-    const int K = static_cast<int>(a.ld / 64);
+    const Tile tile = tile_of(blockIdx.x, static_cast<uint32_t>((a.n + kCols - 1) / kCols), static_cast<uint32_t>((a.T + kTokens - 1) / kTokens));
+    const int64_t c0 = static_cast<int64_t>(tile.c) * kCols, t0 = static_cast<int64_t>(tile.t) * kTokens;
+    const int K = static_cast<int>(a.ld / (64 * WK));
 
     const int8_t* src[L];
 #pragma unroll
     for (int j = 0; j < L; ++j) {
-        const int b = wave * L + j, r = lane >> 2, piece = (lane & 3) ^ ((r >> 1) & 3);
-        src[j] = (b < CT / 16 ? weight_row<GATED>(a, c0, b, r) : token_row<DIG>(a, t0, b - CT / 16, r)) + 16 * piece;
+        const int b = (wave * L + j) % NB, part = (wave * L + j) / NB, r = lane >> 2, piece = (lane & 3) ^ ((r >> 1) & 3);
+        src[j] = (b < CT / 16 ? weight_row<GATED>(a, c0, b, r) : token_row<DIG>(a, t0, b - CT / 16, r)) + 64 * part + 16 * piece;
     }
     const uint32_t base = static_cast<uint32_t>(reinterpret_cast<uintptr_t>(lds));
-    auto request = [&](int k) {
+    uint32_t to = base + wave * L * 1024u, from = 0;   // the slot that the next step is requested into, and the one that is read next
+    const uint32_t to_end = to + S * kSlot;
+    auto request = [&] {
 #pragma unroll
         for (int j = 0; j < L; ++j) {
-            load16_to_lds<false>(base + (k & 3) * kSlot + (wave * L + j) * 1024u, src[j]);
-            src[j] += 64;
+            load16_to_lds<false>(to + j * 1024u, src[j]);
+            src[j] += 64 * WK;
         }
+        to = to + kSlot == to_end ? to_end - S * kSlot : to + kSlot;
     };
     i4 acc[CB][TB];
 #pragma unroll
@@ -162,14 +190,14 @@ __global__ __launch_bounds__(64 * WC * WT) void lordba_i8_product_kernel(Product
         for (int j = 0; j < TB; ++j) acc[i][j] = i4{0, 0, 0, 0};
     i4 fc[2][CB], ft[2][TB];
     const int r = lane & 15, place = 16 * ((lane >> 4) ^ ((r >> 1) & 3));
-    const int8_t* const at_c = lds + wc * CB * 1024 + r * 64 + place;
-    const int8_t* const at_t = lds + (CT / 16 + wt * TB) * 1024 + r * 64 + place;
-    auto read = [&](auto set, int k) {
-        const uint32_t slot = (k & 3) * kSlot;
+    const int8_t* const at_c = lds + wk * kPart + wc * CB * 1024 + r * 64 + place;
+    const int8_t* const at_t = lds + wk * kPart + (CT / 16 + wt * TB) * 1024 + r * 64 + place;
+    auto read = [&](auto set) {
 #pragma unroll
-        for (int i = 0; i < CB; ++i) fc[set.value][i] = *reinterpret_cast<const i4*>(at_c + slot + i * 1024);
+        for (int i = 0; i < CB; ++i) fc[set.value][i] = *reinterpret_cast<const i4*>(at_c + from + i * 1024);
 #pragma unroll
-        for (int i = 0; i < TB; ++i) ft[set.value][i] = *reinterpret_cast<const i4*>(at_t + slot + i * 1024);
+        for (int i = 0; i < TB; ++i) ft[set.value][i] = *reinterpret_cast<const i4*>(at_t + from + i * 1024);
+        from = from + kSlot == S * kSlot ? 0 : from + kSlot;
     };
     auto multiply = [&](auto set) {
 #pragma unroll
@@ -177,55 +205,141 @@ __global__ __launch_bounds__(64 * WC * WT) void lordba_i8_product_kernel(Product
 #pragma unroll
             for (int j = 0; j < TB; ++j) acc[i][j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(fc[set.value][i], ft[set.value][j], acc[i][j], 0, 0, 0);
     };
-    // Everything up to step k + 1 has landed (this wave's loads; steps up to min(k + 3, K - 1) are requested), and this wave's operands are in
-    // registers; then everybody's.
-    auto meet = [&](int k) {
-        if (k + 3 < K) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" :: "n"(2 * L) : "memory");
-        else if (k + 2 < K) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" :: "n"(L) : "memory");
-        else asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+    // Of this wave's loads all but the youngest LATER steps' have landed, and its operands are in registers; then everybody's.  (The builtin, because
+    // the compiler counts the reads of LDS along with it; it does not see the loads.)
+    auto meet = [&](auto later) {
+        constexpr int n = later.value * L;
+        asm volatile("" ::: "memory");
+        __builtin_amdgcn_s_waitcnt((n & 15) | (7 << 4) | ((n >> 4) << 14));
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");
     };
-    using Set0 = std::integral_constant<int, 0>;
-    using Set1 = std::integral_constant<int, 1>;
+    // one operand read between every few products
+    auto weave = [&] {
 #pragma unroll
-    for (int k = 0; k < 4; ++k)
-        if (k < K) request(k);
-    meet(-1);
-    read(Set0{}, 0);
-    for (int k = 0; k < K; k += 2) {   // (K is even)
-        meet(k);
-        if (k + 4 < K) request(k + 4);
-        read(Set1{}, k + 1);
-        multiply(Set0{});
-        meet(k + 1);
-        if (k + 5 < K) request(k + 5);
-        if (k + 2 < K) read(Set0{}, k + 2);
-        multiply(Set1{});
+        for (int i = 0; i < CB + TB; ++i) {
+            __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+            __builtin_amdgcn_sched_group_barrier(0x8, CB * TB / (CB + TB), 0);
+        }
+        __builtin_amdgcn_sched_group_barrier(0x8, CB * TB % (CB + TB), 0);
+        __builtin_amdgcn_sched_barrier(0);
+    };
+    using N0 = std::integral_constant<int, 0>;
+    using N1 = std::integral_constant<int, 1>;
+    using Ring = std::integral_constant<int, S - 2>;
+#pragma unroll
+    for (int k = 0; k < S; ++k)
+        if (k < K) request();
+    if (K >= S) meet(Ring{});
+    else meet(N0{});
+    read(N0{});
+    int k = 0;
+    for (; k + S + 1 < K; k += 2) {
+        meet(Ring{});
+        request();
+        read(N1{});
+        multiply(N0{});
+        weave();
+        meet(Ring{});
+        request();
+        read(N0{});
+        multiply(N1{});
+        weave();
     }
-    finish<CB, TB, DIG, GATED>(a, acc, c0 + wc * (kCols / WC), t0 + wt * (kTokens / WT));
+    // The last steps, S + 1 at most: step k + i + 1 has landed when at most as many are on their way as come behind it.
+    auto last = [&](auto self, auto i) {
+        constexpr int n = i.value;
+        using This = std::integral_constant<int, n & 1>;
+        using Next = std::integral_constant<int, 1 - (n & 1)>;
+        if (k + n + 1 < K) {
+            const int behind = K - 2 - (k + n);
+            if (behind >= S - 2) meet(Ring{});
+            else if (S > 3 && behind == 1) meet(N1{});
+            else meet(N0{});
+            if (k + n + S < K) request();
+            read(Next{});
+        }
+        multiply(This{});
+        if constexpr (n < S)
+            if (k + n + 1 < K) self(self, std::integral_constant<int, n + 1>{});
+    };
+    last(last, N0{});
+    if constexpr (WK > 1) {   // the parts' sums meet in LDS, in the order of the parts
+        static_assert((WK - 1) * CT * TT * 4 <= S * kSlot, "the sums fit the ring");
+        i4* const sums = reinterpret_cast<i4*>(lds) + (wc + WC * wt) * CB * TB * 64 + lane;
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < CB; ++i)
+#pragma unroll
+            for (int j = 0; j < TB; ++j)
+                if (wk > 0) sums[((wk - 1) * WC * WT * CB * TB + i * TB + j) * 64] = acc[i][j];
+        __syncthreads();
+        if (wk > 0) return;
+#pragma unroll
+        for (int p = 0; p < WK - 1; ++p)
+#pragma unroll
+            for (int i = 0; i < CB; ++i)
+#pragma unroll
+                for (int j = 0; j < TB; ++j) acc[i][j] += sums[(p * WC * WT * CB * TB + i * TB + j) * 64];
+    }
+    const int64_t cw = c0 + wc * (kCols / WC), tw = t0 + wt * (kTokens / WT);
+    if (c0 + kCols <= a.n && t0 + kTokens <= a.T) finish<CB, TB, DIG, GATED, true>(a, acc, cw, tw);
+    else finish<CB, TB, DIG, GATED, false>(a, acc, cw, tw);
 }
 
-template <int CT, int TT, int WC, int WT, int DIG, bool GATED>
+template <int CT, int TT, int WC, int WT, int WK, int S, int DIG, bool GATED>
 lordba_status product_launch(const ProductArgs& a, hipStream_t stream) {
     constexpr int kCols = GATED ? CT / 2 : CT, kTokens = TT / DIG;
-    constexpr size_t kLds = 4 * (CT + TT) * 64;
+    constexpr size_t kLds = S * WK * (CT + TT) * 64;
     static_assert(kLds <= 160 * 1024, "LDS of a compute unit");
     if constexpr (kLds > 64 * 1024) {
-        if (hipFuncSetAttribute(reinterpret_cast<const void*>(lordba_i8_product_kernel<CT, TT, WC, WT, DIG, GATED>),
+        if (hipFuncSetAttribute(reinterpret_cast<const void*>(lordba_i8_product_kernel<CT, TT, WC, WT, WK, S, DIG, GATED>),
                                 hipFuncAttributeMaxDynamicSharedMemorySize, kLds) != hipSuccess) {
             (void)hipGetLastError();
             return LORDBA_ERR_LAUNCH;
         }
     }
-    const dim3 grid(static_cast<unsigned>((a.n + kCols - 1) / kCols), static_cast<unsigned>((a.T + kTokens - 1) / kTokens));
-    hipLaunchKernelGGL((lordba_i8_product_kernel<CT, TT, WC, WT, DIG, GATED>), grid, dim3(64 * WC * WT), kLds, stream, a);
+    const int64_t tiles = (a.n + kCols - 1) / kCols * ((a.T + kTokens - 1) / kTokens);
+    if (tiles > INT32_MAX) return LORDBA_ERR_DIM;
+    const dim3 grid(static_cast<unsigned>(tiles));
+    hipLaunchKernelGGL((lordba_i8_product_kernel<CT, TT, WC, WT, WK, S, DIG, GATED>), grid, dim3(64 * WC * WT * WK), kLds, stream, a);
     return i8_launched();
+}
+
+// The tiles and what a step of 64 columns of one takes on a compute unit, in nanoseconds: alone on a chip with few workgroups (waiting), and as a
+// share of a chip that is full (throughput; small tiles run side by side on a unit).  Measured on square and ragged shapes of 1 to 16384 rows;
+// the sum below is within 30 % of what a call takes and picks the fastest tile or one within 10 % of it on all of those.
+struct TileCost {
+    int channels, tokens;
+    double alone, share;
+};
+constexpr TileCost kTiles[] = {{256, 256, 600, 800}, {256, 128, 390, 510}, {128, 128, 200, 300}, {64, 64, 77, 125}, {32, 32, 35, 60}, {32, 16, 25, 50}};
+constexpr TileCost kGatedTiles[] = {{256, 256, 600, 800}, {256, 128, 390, 510}, {128, 128, 200, 300}, {64, 64, 77, 125}, {64, 32, 60, 105}, {64, 16, 40, 100}};
+
+int cheapest_tile(const TileCost (&tiles)[6], int64_t channels, int64_t rows, bool two_digits) {
+    int best = 0;
+    double least = 0;
+    for (int i = 0; i < (two_digits ? 5 : 6); ++i) {   // (two digits are two blocks of 16 rows)
+        const double n = static_cast<double>((channels + tiles[i].channels - 1) / tiles[i].channels) * static_cast<double>((rows + tiles[i].tokens - 1) / tiles[i].tokens);
+        const double rounds = n <= 256 ? n / 256 : std::ceil(n / 256);   // (256 compute units)
+        const double cost = std::max(tiles[i].alone, rounds * tiles[i].share);
+        if (i == 0 || cost < least) best = i, least = cost;
+    }
+    return best;
 }
 
 template <int DIG, bool GATED>
 lordba_status product(const ProductArgs& a, hipStream_t stream) {
-    return product_launch<64, 64, 2, 2, DIG, GATED>(a, stream);
+    switch (cheapest_tile(GATED ? kGatedTiles : kTiles, (GATED ? 2 : 1) * a.n, DIG * a.T, DIG == 2)) {
+        case 0: return product_launch<256, 256, 4, 2, 1, 4, DIG, GATED>(a, stream);
+        case 1: return product_launch<256, 128, 4, 2, 1, 4, DIG, GATED>(a, stream);
+        case 2: return product_launch<128, 128, 2, 4, 1, 4, DIG, GATED>(a, stream);
+        case 3: return product_launch<64, 64, GATED ? 1 : 2, 2, 2, 4, DIG, GATED>(a, stream);
+        case 4: return product_launch<GATED ? 64 : 32, 32, 1, 1, GATED ? 2 : 4, 4, DIG, GATED>(a, stream);
+        default:
+            if constexpr (DIG == 1) return product_launch<GATED ? 64 : 32, 16, 1, 1, GATED ? 2 : 4, 4, DIG, GATED>(a, stream);
+            return LORDBA_ERR_LAUNCH;   // (cheapest_tile does not name it)
+    }
 }
 
 // What the four entry points check alike.

@@ -304,7 +304,7 @@ def test_no_rows(torch):
     dx, dgu = binding.lordba_gated_i8_backward(e(0, 5), e(2, 0, 5), Wt, s)
     assert dx.shape == (0, 20) and dgu.shape == (2, 0, 5)
     q, sc = binding.lordba_quantize_rows(e(0, 20))
-    assert q.shape == (0, 128) and sc.shape == (0,)
+    assert q.shape == (0, binding.lordba_i8_row_bytes(20)) and sc.shape == (0,)
 
 
 def test_results_pass_the_range_of_fp16_as_infinities(torch):
@@ -332,7 +332,7 @@ def test_matrices_past_4_gib(torch):
     # weights, rows, and results whose bytes pass 32 bits: sampled entries
     n, k = (1 << 25) // 8 + 40, 1025
     gen = torch.Generator(device="cuda").manual_seed(1)
-    W = torch.randint(-127, 128, (n, 1152), generator=gen, device="cuda", dtype=torch.int8)
+    W = torch.randint(-127, 128, (n, 1280), generator=gen, device="cuda", dtype=torch.int8)
     assert W.shape[1] == binding.lordba_i8_row_bytes(k) and W.numel() > 1 << 32
     W[:, k:] = 0
     ws = torch.full((n,), 1e-3, device="cuda")

@@ -14,7 +14,7 @@ def lib():
 
 
 def test_sizes(lib):
-    assert [binding.lordba_i8_row_bytes(c) for c in (1, 128, 129, 4096, 131071)] == [128, 128, 256, 4096, 131072]
+    assert [binding.lordba_i8_row_bytes(c) for c in (1, 128, 129, 4096, 131071)] == [256, 256, 256, 4096, 131072]
     assert [binding.lordba_i8_row_bytes(c) for c in (0, -1, 131072)] == [0, 0, 0]
     assert binding.lordba_i8_workspace_bytes(3, 200, 1) >= 3 * 256 + 12
     assert binding.lordba_i8_workspace_bytes(3, 200, 2) >= 6 * 256 + 12
