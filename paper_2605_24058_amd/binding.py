@@ -931,6 +931,9 @@ def lordba_quantize_rows(x, col_scale=None, digits: int = 1, stream=None):
 def lordba_linear_i8(x, W, w_scale, digits: int = 1, y_out=None, workspace=None, stream=None):
     """The frozen base projection y = x W^T on 8-bit weights: x fp16 [T, d_in], W the layout of int8 [d_out, d_in], w_scale fp32
     [d_out]; the rows of x in one digit (8 bits) or two (16).  Returns y fp16 [T, d_out], what lordba_forward takes as y_base."""
+    res = _plain_call("linear_i8", x, W, w_scale, digits, y_out, workspace, stream)
+    if res is not None:
+        return res
     import torch
 
     lib = load_library()
@@ -955,6 +958,9 @@ def lordba_linear_i8(x, W, w_scale, digits: int = 1, y_out=None, workspace=None,
 def lordba_linear_i8_backward(g, Wt, w_scale, digits: int = 2, dx_out=None, workspace=None, stream=None):
     """The gradient of that projection with respect to x: g fp16 [T, d_out], Wt the transposed layout of W, w_scale fp32 [d_out];
     g * w_scale in two digits unless asked otherwise.  Returns dx fp16 [T, d_in], what lordba_backward takes as dx_base."""
+    res = _plain_call("linear_i8_backward", g, Wt, w_scale, digits, dx_out, workspace, stream)
+    if res is not None:
+        return res
     import torch
 
     lib = load_library()
@@ -980,6 +986,9 @@ def lordba_gated_i8(x, W, w_scale, addends=None, digits: int = 1, save: bool = F
     """h = silu(x Wg^T + addends[0]) * (x Wu^T + addends[1]) on 8-bit weights: x fp16 [T, d_in]; W the layout of int8 [2 d_ff, d_in],
     gate's rows first; w_scale fp32 [2 d_ff]; addends fp16 [2, T, d_ff]: the branches of the two projections' adapters.
     Returns h fp16 [T, d_ff]; save: (h, gate_up) with gate_up fp16 [2, T, d_ff] for lordba_gated_i8_backward."""
+    res = _plain_call("gated_i8", x, W, w_scale, addends, digits, save, workspace, stream)
+    if res is not None:
+        return res
     import torch
 
     lib = load_library()
@@ -1010,6 +1019,9 @@ def lordba_gated_i8(x, W, w_scale, addends=None, digits: int = 1, save: bool = F
 def lordba_gated_i8_backward(dh, gate_up, Wt, w_scale, digits: int = 2, workspace=None, stream=None):
     """Backward pass of lordba_gated_i8: dh fp16 [T, d_ff], the kept gate_up, Wt the transposed layout of the [2 d_ff, d_in] weights.
     Returns (dx fp16 [T, d_in], dgate_up fp16 [2, T, d_ff]); dgate_up holds the upstream gradients of the two adapters."""
+    res = _plain_call("gated_i8_backward", dh, gate_up, Wt, w_scale, digits, workspace, stream)
+    if res is not None:
+        return res
     import torch
 
     lib = load_library()
@@ -1035,6 +1047,9 @@ def lordba_dropout(x, p: float, seed: int, offset: int = 0, y_base=None, y_out=N
     """y = y_base + dropout(x): elements are dropped at probability p (a multiple of 1/65536), the kept ones divided by the exact kept share;
     the mask follows from (seed, offset + offset_dev) and the element's index.  The backward pass is the same call on the gradient.
     x fp16 of any shape; y_base like x or None; offset_dev: int64 CUDA tensor of one element or None."""
+    res = _plain_call("dropout", x, p, seed, offset, y_base, y_out, offset_dev, stream)
+    if res is not None:
+        return res
     import torch
 
     lib = load_library()

@@ -35,23 +35,44 @@ __device__ __forceinline__ RowScale scale_of(uint32_t max_bits, float D) {
     return {D / amax, amax / D};
 }
 
-// Eight numbers into their digits: bytes 0..7 of (hi, lo); with one digit all of it in hi.
+// Eight numbers into their digits: bytes 0..7 of (hi, lo); with one digit all of it in hi.  Adding 1.5 * 2^23 rounds to an integer (ties to even) and
+// leaves it in two's complement in the low bits of the sum; a byte permutation gathers the bytes of four sums.
 template <int DIG>
 __device__ __forceinline__ void digits_of(const float (&v)[8], float inverse, uint2& hi, uint2& lo) {
-    uint32_t h[2] = {0, 0}, l[2] = {0, 0};
+    uint32_t b[8];
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
-        // (a row without a number has inverse 0: infinity times that is a NaN, whose conversion is 0)
-        const int q = static_cast<int>(rintf(inverse == 0.f ? 0.f : v[e] * inverse));
-        if constexpr (DIG == 1) {
-            h[e >> 2] |= static_cast<uint32_t>(q & 0xFF) << (8 * (e & 3));
-        } else {
-            h[e >> 2] |= static_cast<uint32_t>(((q + 128) >> 8) & 0xFF) << (8 * (e & 3));
-            l[e >> 2] |= static_cast<uint32_t>(q & 0xFF) << (8 * (e & 3));
-        }
+        float q = v[e] * inverse;
+        asm("" : "+v"(q));   // (two roundings, as the definition has it: not one fused operation)
+        b[e] = __float_as_uint(q + 12582912.f);
     }
-    hi = make_uint2(h[0], h[1]);
-    lo = make_uint2(l[0], l[1]);
+    auto gather = [](uint32_t b0, uint32_t b1, uint32_t b2, uint32_t b3, uint32_t pair) {   // byte `pair & 0xFF` of each
+        return __builtin_amdgcn_perm(__builtin_amdgcn_perm(b3, b2, pair), __builtin_amdgcn_perm(b1, b0, pair), 0x05040100u);
+    };
+    const bool none = inverse == 0.f;   // (a row of zeros, or without a number: infinity times zero is no zero)
+    if constexpr (DIG == 1) {
+        hi = make_uint2(gather(b[0], b[1], b[2], b[3], 0x0400u), gather(b[4], b[5], b[6], b[7], 0x0400u));
+    } else {
+        lo = make_uint2(gather(b[0], b[1], b[2], b[3], 0x0400u), gather(b[4], b[5], b[6], b[7], 0x0400u));
+#pragma unroll
+        for (int e = 0; e < 8; ++e) b[e] += 128;
+        hi = make_uint2(gather(b[0], b[1], b[2], b[3], 0x0501u), gather(b[4], b[5], b[6], b[7], 0x0501u));
+        lo = none ? make_uint2(0, 0) : lo;
+    }
+    hi = none ? make_uint2(0, 0) : hi;
+}
+
+// Eight channel scales from column c on, zeros from column `cols` on.
+__device__ __forceinline__ void load_scales(const float* p, int64_t c, int64_t cols, float (&v)[8]) {
+    typedef float f4_any __attribute__((ext_vector_type(4), aligned(4)));
+    if (c + 8 <= cols) {
+        const f4_any a = *reinterpret_cast<const f4_any*>(p + c), b = *reinterpret_cast<const f4_any*>(p + c + 4);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] = a[e], v[4 + e] = b[e];
+    } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] = c + e < cols ? p[c + e] : 0.f;
+    }
 }
 
 // Eight numbers of a row from column c on, zeros from column `cols` on.
@@ -81,31 +102,34 @@ struct QuantizeArgs {
     int64_t rows, cols, ld;
 };
 
+// NV > 0: a thread's numbers stay in registers between the two passes over the row; NV = 0 (more than 32768 columns): they are read again.
 template <int TPR, int NV, int DIG, bool CS>
 __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void lordba_quantize_rows_kernel(QuantizeArgs a) {
     const int t = threadIdx.x % TPR;
     const int64_t row = TPR < 256 ? static_cast<int64_t>(blockIdx.x) * (256 / TPR) + threadIdx.x / TPR : blockIdx.x;
     if (row >= a.rows) return;   // (whole waves: a wave has one row)
     const _Float16* x = a.x + row * a.cols;
-    u4 raw[NV];
+    const int turns = NV > 0 ? NV : static_cast<int>((a.ld + 8 * TPR - 1) / (8 * TPR));
+    u4 raw[NV > 0 ? NV : 1];
+    if constexpr (NV > 0) {
 #pragma unroll
-    for (int i = 0; i < NV; ++i) {
-        const int64_t c = 8 * static_cast<int64_t>(t + i * TPR);
-        raw[i] = c < a.cols ? load_part(x, c, a.cols) : u4{0u, 0u, 0u, 0u};
+        for (int i = 0; i < NV; ++i) {
+            const int64_t c = 8 * static_cast<int64_t>(t + i * TPR);
+            raw[i] = c < a.cols ? load_part(x, c, a.cols) : u4{0u, 0u, 0u, 0u};
+        }
     }
     // (with column scales the products are formed again for the second use: kept, they would take twice the registers of the row)
     auto numbers = [&](int i, float (&f)[8]) {
         const int64_t c = 8 * static_cast<int64_t>(t + i * TPR);
-        const h8 h = as_h8(raw[i]);
+        const h8 h = as_h8(NV > 0 ? raw[NV > 0 ? i : 0] : c < a.cols ? load_part(x, c, a.cols) : u4{0u, 0u, 0u, 0u});
+        float s[8];
+        if constexpr (CS) load_scales(a.col_scale, c, a.cols, s);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            f[e] = static_cast<float>(h[e]);
-            if constexpr (CS) f[e] *= c + e < a.cols ? a.col_scale[c + e] : 0.f;
-        }
+        for (int e = 0; e < 8; ++e) f[e] = CS ? static_cast<float>(h[e]) * s[e] : static_cast<float>(h[e]);
     };
     uint32_t m = 0;
-#pragma unroll
-    for (int i = 0; i < NV; ++i) {
+#pragma unroll NV > 0 ? NV : 1
+    for (int i = 0; i < turns; ++i) {
         float f[8];
         numbers(i, f);
 #pragma unroll
@@ -113,8 +137,8 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void lordba_quantize_rows_ke
     }
     const RowScale s = scale_of(row_max<TPR>(m), DIG == 1 ? 127.f : 32512.f);
     if (t == 0) a.scale[row] = s.scale;
-#pragma unroll
-    for (int i = 0; i < NV; ++i) {
+#pragma unroll NV > 0 ? NV : 1
+    for (int i = 0; i < turns; ++i) {
         const int64_t c = 8 * static_cast<int64_t>(t + i * TPR);
         if (c >= a.ld) break;
         float f[8];
@@ -144,7 +168,7 @@ lordba_status quantize(const QuantizeArgs& a, hipStream_t stream) {
     if (vectors <= 1024) return quantize_launch<256, 4, DIG, CS>(a, stream);
     if (vectors <= 2048) return quantize_launch<512, 4, DIG, CS>(a, stream);
     if (vectors <= 4096) return quantize_launch<1024, 4, DIG, CS>(a, stream);
-    return quantize_launch<1024, 16, DIG, CS>(a, stream);
+    return quantize_launch<1024, 0, DIG, CS>(a, stream);
 }
 
 // ---- the gradient of h = g sigma(g) u -----------------------------------------------------------------------------
@@ -164,7 +188,7 @@ __device__ __forceinline__ void gated_grad(h8 dh, h8 gate, h8 up, float (&dg)[8]
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
         const float g = static_cast<float>(gate[e]), u = static_cast<float>(up[e]), d = static_cast<float>(dh[e]);
-        const float sigma = 1.f / (1.f + __expf(-g));
+        const float sigma = __builtin_amdgcn_rcpf(1.f + __expf(-g));   // (to one last place)
         dg[e] = d * u * sigma * (1.f + g * (1.f - sigma));
         du[e] = d * g * sigma;
     }
@@ -198,12 +222,15 @@ __global__ __launch_bounds__(TPR) void lordba_gated_grad_kernel(GatedGradArgs a)
         float dg[8], du[8];
         gated_grad(as_h8(load_part(dh, c, F)), as_h8(load_part(gate, c, F)), as_h8(load_part(up, c, F)), dg, du);
         h8 hg, hu;
+        float sg[8], su[8];
+        load_scales(a.w_scale, c, F, sg);
+        load_scales(a.w_scale + F, c, F, su);
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
             hg[e] = static_cast<_Float16>(dg[e]);
             hu[e] = static_cast<_Float16>(du[e]);
-            dg[e] *= c + e < F ? a.w_scale[c + e] : 0.f;
-            du[e] *= c + e < F ? a.w_scale[F + c + e] : 0.f;
+            dg[e] *= sg[e];
+            du[e] *= su[e];
             m = max(m, max(__float_as_uint(dg[e]) & 0x7FFFFFFFu, __float_as_uint(du[e]) & 0x7FFFFFFFu));
             if constexpr (NV > 0) {
                 v[i][0][e] = dg[e];
@@ -227,11 +254,11 @@ __global__ __launch_bounds__(TPR) void lordba_gated_grad_kernel(GatedGradArgs a)
             for (int e = 0; e < 8; ++e) dg[e] = v[i][0][e], du[e] = v[i][1][e];
         } else {
             gated_grad(as_h8(load_part(dh, c, F)), as_h8(load_part(gate, c, F)), as_h8(load_part(up, c, F)), dg, du);
+            float sg[8], su[8];
+            load_scales(a.w_scale, c, F, sg);
+            load_scales(a.w_scale + F, c, F, su);
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                dg[e] *= c + e < F ? a.w_scale[c + e] : 0.f;
-                du[e] *= c + e < F ? a.w_scale[F + c + e] : 0.f;
-            }
+            for (int e = 0; e < 8; ++e) dg[e] *= sg[e], du[e] *= su[e];
         }
         uint2 hi, lo;
         digits_of<DIG>(dg, s.inverse, hi, lo);

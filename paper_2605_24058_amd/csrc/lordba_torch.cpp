@@ -319,10 +319,143 @@ PyObject* backward_multi(PyObject*, PyObject* const* a, Py_ssize_t n) {
     END_HANDLE_TH_ERRORS
 }
 
+// ---- 8-bit projections, the gated block, dropout.  Outputs and workspaces are made on the current stream, which the call runs on: with another one
+// the binding makes them there.
+constexpr at::ScalarType kI8 = at::kChar;
+
+// W is the layout of an int8 matrix [rows, cols]
+bool laid_out(const at::Tensor* W, int64_t rows, int64_t cols) {
+    return W->dim() == 2 && W->size(0) == rows && W->size(1) == static_cast<int64_t>(lordba_i8_row_bytes(cols));
+}
+bool digits_of(PyObject* o, int64_t T, int64_t cols, int* digits, size_t* bytes) {
+    if (!PyLong_CheckExact(o)) return false;
+    const long d = PyLong_AsLong(o);
+    if (d != 1 && d != 2) { PyErr_Clear(); return false; }
+    *digits = static_cast<int>(d);
+    *bytes = lordba_i8_workspace_bytes(T, cols, *digits);
+    return true;
+}
+// an output or a workspace: an argument, or None for a new one
+bool tensor_or_new(PyObject* o, at::ScalarType type, const at::Tensor* like, at::IntArrayRef shape, bool any_shape, at::Tensor* out) {
+    if (o == Py_None) {
+        *out = at::empty(shape, at::TensorOptions().dtype(type).device(like->device()));
+        return true;
+    }
+    const at::Tensor* t = plain(o, type);
+    if (!t || (!any_shape && t->sizes() != shape)) return false;
+    *out = *t;
+    return true;
+}
+
+// (x, W, w_scale, digits, y_out, workspace, stream), and the same of the gradient with (g, Wt, ...)
+PyObject* linear_any(PyObject* const* a, Py_ssize_t n, bool backward) {
+    NEED(n == 7 && unwatched() && a[6] == Py_None);
+    const at::Tensor *x = plain(a[0], kF16), *W = plain(a[1], kI8), *s = plain(a[2], kF32);
+    NEED(x && W && s && x->dim() == 2 && W->dim() == 2);
+    const int64_t T = x->size(0), contracted = x->size(1), out = W->size(0);
+    NEED(s->numel() == (backward ? contracted : out) && laid_out(W, out, contracted));
+    int digits;
+    size_t bytes;
+    void* st;
+    at::Tensor y, ws;
+    NEED(digits_of(a[3], T, contracted, &digits, &bytes) && stream_of(a[6], x, &st));
+    NEED(tensor_or_new(a[4], kF16, x, {T, out}, false, &y) &&
+         tensor_or_new(a[5], at::kByte, x, {static_cast<int64_t>(bytes < 16 ? 16 : bytes)}, true, &ws));
+    const int rc = backward ? unlocked(lordba_linear_i8_backward, ptr<void>(x), ptr<int8_t>(W), ptr<float>(s), ptr<void>(y), ptr<void>(ws),
+                                       static_cast<size_t>(ws.numel()), T, out, contracted, digits, st)
+                            : unlocked(lordba_linear_i8, ptr<void>(x), ptr<int8_t>(W), ptr<float>(s), ptr<void>(y), ptr<void>(ws),
+                                       static_cast<size_t>(ws.numel()), T, contracted, out, digits, st);
+    return result(y, rc);
+}
+PyObject* linear_i8(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    HANDLE_TH_ERRORS
+    return linear_any(a, n, false);
+    END_HANDLE_TH_ERRORS
+}
+PyObject* linear_i8_backward(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    HANDLE_TH_ERRORS
+    return linear_any(a, n, true);
+    END_HANDLE_TH_ERRORS
+}
+
+PyObject* pair(const at::Tensor& u, const at::Tensor& v) {
+    PyObject* out = PyTuple_New(2);
+    if (out) {
+        PyTuple_SET_ITEM(out, 0, THPVariable_Wrap(u));
+        PyTuple_SET_ITEM(out, 1, THPVariable_Wrap(v));
+    }
+    return out;
+}
+
+// (x, W, w_scale, addends, digits, save, workspace, stream)
+PyObject* gated_i8(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    HANDLE_TH_ERRORS
+    NEED(n == 8 && unwatched() && a[7] == Py_None && (a[5] == Py_True || a[5] == Py_False));
+    const at::Tensor *x = plain(a[0], kF16), *W = plain(a[1], kI8), *s = plain(a[2], kF32), *add = a[3] == Py_None ? nullptr : plain(a[3], kF16);
+    NEED(x && W && s && (add || a[3] == Py_None) && x->dim() == 2 && s->numel() % 2 == 0);
+    const int64_t T = x->size(0), d_in = x->size(1), F = s->numel() / 2;
+    NEED(laid_out(W, 2 * F, d_in) && (!add || shaped(add, {2, T, F})));
+    int digits;
+    size_t bytes;
+    void* st;
+    at::Tensor ws, kept;
+    NEED(digits_of(a[4], T, d_in, &digits, &bytes) && stream_of(a[7], x, &st) &&
+         tensor_or_new(a[6], at::kByte, x, {static_cast<int64_t>(bytes < 16 ? 16 : bytes)}, true, &ws));
+    const at::Tensor h = empty(x, kF16, {T, F});
+    if (a[5] == Py_True) kept = empty(x, kF16, {2, T, F});
+    const int rc = unlocked(lordba_gated_i8, ptr<void>(x), ptr<int8_t>(W), ptr<float>(s), ptr<void>(add), ptr<void>(h),
+                            kept.defined() ? ptr<void>(kept) : nullptr, ptr<void>(ws), static_cast<size_t>(ws.numel()), T, d_in, F, digits, st);
+    return rc == LORDBA_OK && kept.defined() ? pair(h, kept) : result(h, rc);
+    END_HANDLE_TH_ERRORS
+}
+
+// (dh, gate_up, Wt, w_scale, digits, workspace, stream)
+PyObject* gated_i8_backward(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    HANDLE_TH_ERRORS
+    NEED(n == 7 && unwatched() && a[6] == Py_None);
+    const at::Tensor *dh = plain(a[0], kF16), *gu = plain(a[1], kF16), *Wt = plain(a[2], kI8), *s = plain(a[3], kF32);
+    NEED(dh && gu && Wt && s && dh->dim() == 2 && Wt->dim() == 2);
+    const int64_t T = dh->size(0), F = dh->size(1), d_in = Wt->size(0);
+    NEED(shaped(gu, {2, T, F}) && s->numel() == 2 * F && laid_out(Wt, d_in, 2 * F));
+    int digits;
+    size_t bytes;
+    void* st;
+    at::Tensor ws;
+    NEED(digits_of(a[4], T, 2 * F, &digits, &bytes) && stream_of(a[6], dh, &st) &&
+         tensor_or_new(a[5], at::kByte, dh, {static_cast<int64_t>(bytes < 16 ? 16 : bytes)}, true, &ws));
+    const at::Tensor dx = empty(dh, kF16, {T, d_in}), dgu = empty(dh, kF16, {2, T, F});
+    const int rc = unlocked(lordba_gated_i8_backward, ptr<void>(dh), ptr<void>(gu), ptr<int8_t>(Wt), ptr<float>(s), ptr<void>(dx), ptr<void>(dgu),
+                            ptr<void>(ws), static_cast<size_t>(ws.numel()), T, d_in, F, digits, st);
+    return rc == LORDBA_OK ? pair(dx, dgu) : PyLong_FromLong(rc);
+    END_HANDLE_TH_ERRORS
+}
+
+// (x, p, seed, offset, y_base, y_out, offset_dev, stream)
+PyObject* dropout(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    HANDLE_TH_ERRORS
+    NEED(n == 8 && unwatched() && a[7] == Py_None && PyFloat_CheckExact(a[1]) && PyLong_CheckExact(a[2]) && PyLong_CheckExact(a[3]));
+    const at::Tensor *x = plain(a[0], kF16), *b = a[4] == Py_None ? nullptr : plain(a[4], kF16), *dev = a[6] == Py_None ? nullptr : plain(a[6], at::kLong);
+    NEED(x && (b || a[4] == Py_None) && (dev || a[6] == Py_None) && (!b || b->sizes() == x->sizes()) && (!dev || dev->numel() == 1));
+    const uint64_t seed = PyLong_AsUnsignedLongLong(a[2]), offset = PyLong_AsUnsignedLongLong(a[3]);
+    if (PyErr_Occurred()) {   // (negative, or more than 64 bits)
+        PyErr_Clear();
+        Py_RETURN_NONE;
+    }
+    void* st;
+    at::Tensor y;
+    NEED(stream_of(a[7], x, &st) && tensor_or_new(a[5], kF16, x, x->sizes(), false, &y));
+    const int rc = unlocked(lordba_dropout, ptr<void>(x), ptr<void>(b), ptr<void>(y), x->numel(), PyFloat_AS_DOUBLE(a[1]), seed, offset,
+                            ptr<uint64_t>(dev), st);
+    return result(y, rc);
+    END_HANDLE_TH_ERRORS
+}
+
 #define METHOD(name) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(name)), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {METHOD(forward),        METHOD(forward_multi),        METHOD(forward_batched), METHOD(forward_batched_multi),
                          METHOD(pack_latents),   METHOD(forward_save_t),       METHOD(forward_multi_save_t),
-                         METHOD(backward),       METHOD(backward_multi),       {nullptr, nullptr, 0, nullptr}};
+                         METHOD(backward),       METHOD(backward_multi),       METHOD(linear_i8),
+                         METHOD(linear_i8_backward), METHOD(gated_i8),           METHOD(gated_i8_backward), METHOD(dropout),
+                         {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_lordba_torch", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace
