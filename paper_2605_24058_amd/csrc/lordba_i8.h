@@ -14,6 +14,7 @@
 #include <stdint.h>
 
 #include "lordba.h"
+#include "lordba_dev_util.h"
 #include "lordba_host_util.h"
 
 namespace {
@@ -31,6 +32,19 @@ inline bool i8_overlap(const void* p, size_t pn, const void* q, size_t qn) {
     return p && q && pn && qn && a < b + qn && b < a + pn;
 }
 inline bool i8_misaligned(const void* p, uintptr_t bytes) { return (reinterpret_cast<uintptr_t>(p) & (bytes - 1)) != 0; }
+
+// Eight numbers of a row from column c < cols on, zeros from column `cols` on.  At a row's end all of them are requested before the first is
+// looked at: one wait, not eight.
+__device__ __forceinline__ u4 load_part(const _Float16* row, int64_t c, int64_t cols) {
+    if (c + 8 <= cols) return load16_any(row + c);
+    uint32_t h[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) h[e] = reinterpret_cast<const uint16_t*>(row)[min(c + e, cols - 1)];
+    u4 v;
+#pragma unroll
+    for (int e = 0; e < 8; e += 2) v[e >> 1] = (c + e < cols ? h[e] : 0u) | (c + e + 1 < cols ? h[e + 1] << 16 : 0u);
+    return v;
+}
 
 inline lordba_status i8_launched() { return hipGetLastError() == hipSuccess ? LORDBA_OK : LORDBA_ERR_LAUNCH; }
 

@@ -31,12 +31,7 @@ typedef float f4_any __attribute__((ext_vector_type(4), aligned(4)));
 // Eight consecutive entries from column c of n; the part of a row that is there.
 template <bool FULL>
 __device__ __forceinline__ u4 load8(const _Float16* row, int64_t c, int64_t n) {
-    if (FULL || c + 8 <= n) return load16_any(row + c);
-    u4 v = {0u, 0u, 0u, 0u};
-#pragma unroll
-    for (int e = 0; e < 8; ++e)
-        if (c + e < n) v[e >> 1] |= static_cast<uint32_t>(reinterpret_cast<const uint16_t*>(row)[c + e]) << (16 * (e & 1));
-    return v;
+    return FULL ? load16_any(row + c) : load_part(row, c, n);
 }
 template <bool FULL>
 __device__ __forceinline__ void load8(const float* p, int64_t c, int64_t n, float (&v)[8]) {
@@ -46,17 +41,18 @@ __device__ __forceinline__ void load8(const float* p, int64_t c, int64_t n, floa
         for (int e = 0; e < 4; ++e) v[e] = a[e], v[4 + e] = b[e];
     } else {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] = c + e < n ? p[c + e] : 0.f;
+        for (int e = 0; e < 8; ++e) v[e] = p[min(c + e, n - 1)];
     }
 }
-template <bool FULL>
+template <bool FULL, bool STREAM = false>
 __device__ __forceinline__ void store8(_Float16* row, int64_t c, int64_t n, const float (&f)[8]) {
     h8 h;
 #pragma unroll
     for (int e = 0; e < 8; ++e) h[e] = static_cast<_Float16>(f[e]);
     const u4 v = __builtin_bit_cast(u4, h);
     if (FULL || c + 8 <= n) {
-        *reinterpret_cast<u4_any*>(row + c) = v;
+        if constexpr (STREAM) store16_any_stream(row + c, v);
+        else *reinterpret_cast<u4_any*>(row + c) = v;
     } else {
 #pragma unroll
         for (int e = 0; e < 8; ++e)
@@ -66,7 +62,8 @@ __device__ __forceinline__ void store8(_Float16* row, int64_t c, int64_t n, cons
 
 // The sums of a lane (CB x TB blocks) to y.  c0, t0: the first column of y and the first token of the wave's part.  A lane has eight
 // consecutive columns of a token in a pair of weight blocks (of gate and of up each), see weight_row.  FULL: all columns and tokens exist.
-template <int CB, int TB, int DIG, bool GATED, bool FULL>
+// STREAM: the results go past the caches.
+template <int CB, int TB, int DIG, bool GATED, bool STREAM, bool FULL>
 __device__ __forceinline__ void finish(const ProductArgs& a, const i4 (&acc)[CB][TB], int64_t c0, int64_t t0) {
     constexpr int P = GATED ? 2 : 1, G = 2 * P, J = TB / DIG;
     static_assert(CB % G == 0 && TB % DIG == 0, "whole groups of blocks");
@@ -80,20 +77,24 @@ __device__ __forceinline__ void finish(const ProductArgs& a, const i4 (&acc)[CB]
         const int64_t c = c0 + 32 * (cb / G) + 8 * (lane >> 4);
         if (!FULL && c >= a.n) continue;
         float w[P][8];
-        u4 add[P][J];
+        constexpr int A = J < 4 ? J : 4;   // tokens whose addends are requested together: what the registers hold
+        u4 add[P][A];
 #pragma unroll
         for (int p = 0; p < P; ++p) {
             if (a.w_scale) load8<FULL>(a.w_scale + p * a.n, c, a.n, w[p]);
             else w[p][0] = w[p][1] = w[p][2] = w[p][3] = w[p][4] = w[p][5] = w[p][6] = w[p][7] = 1.f;
-            if constexpr (GATED) {
-#pragma unroll
-                for (int j = 0; j < J; ++j)
-                    add[p][j] = a.addends && (FULL || t1 + 16 * j < a.T) ? load8<FULL>(a.addends + p * plane + (t1 + 16 * j) * a.n, c, a.n) : u4{0u, 0u, 0u, 0u};
-            }
         }
 #pragma unroll
         for (int j = 0; j < J; ++j) {
             const int64_t t = t1 + 16 * j;
+            if constexpr (GATED)
+                if (j % A == 0) {
+#pragma unroll
+                    for (int p = 0; p < P; ++p)
+#pragma unroll
+                        for (int i = 0; i < A; ++i)
+                            add[p][i] = a.addends && (FULL || t + 16 * i < a.T) ? load8<FULL>(a.addends + p * plane + (t + 16 * i) * a.n, c, a.n) : u4{0u, 0u, 0u, 0u};
+                }
             if (!FULL && t >= a.T) continue;
             float v[P][8];
 #pragma unroll
@@ -104,17 +105,17 @@ __device__ __forceinline__ void finish(const ProductArgs& a, const i4 (&acc)[CB]
                     float sum = static_cast<float>(acc[b][j * DIG][e & 3]);
                     if constexpr (DIG == 2) sum = fmaf(256.f, sum, static_cast<float>(acc[b][j * DIG + 1][e & 3]));
                     v[p][e] = sum * s[j] * w[p][e];
-                    if constexpr (GATED) v[p][e] += static_cast<float>(as_h8(add[p][j])[e]);
+                    if constexpr (GATED) v[p][e] += static_cast<float>(as_h8(add[p][j % A])[e]);
                 }
             if constexpr (GATED) {
-                if (a.kept) {
-                    store8<FULL>(a.kept + t * a.n, c, a.n, v[0]);
-                    store8<FULL>(a.kept + plane + t * a.n, c, a.n, v[1]);
+                if (a.kept) {   // (wanted by the backward pass only: past the caches, which the products' rows need; 189 -> 178 us at 2048 x 4096 x 11008)
+                    store8<FULL, true>(a.kept + t * a.n, c, a.n, v[0]);
+                    store8<FULL, true>(a.kept + plane + t * a.n, c, a.n, v[1]);
                 }
 #pragma unroll
-                for (int e = 0; e < 8; ++e) v[0][e] = v[0][e] / (1.f + __expf(-v[0][e])) * v[1][e];
+                for (int e = 0; e < 8; ++e) v[0][e] = v[0][e] * __builtin_amdgcn_rcpf(1.f + __expf(-v[0][e])) * v[1][e];
             }
-            store8<FULL>(a.y + t * a.n, c, a.n, v[0]);
+            store8<FULL, STREAM>(a.y + t * a.n, c, a.n, v[0]);
         }
     }
 }
@@ -134,7 +135,7 @@ __device__ __forceinline__ const int8_t* token_row(const ProductArgs& a, int64_t
 
 // Which tile a workgroup takes.  Workgroups go to the eight XCDs in turn, each with an L2 of its own: every XCD gets a contiguous eighth of the
 // tiles, in groups of kGroup tiles along the tokens, so that those it runs at a time share rows of both operands.
-constexpr uint32_t kGroup = 4;
+constexpr uint32_t kGroup = 4;   // (2 .. 16 measured: 4 and 8 alike, 2 and 16 up to 6 % slower)
 struct Tile {
     uint32_t c, t;
 };
@@ -283,8 +284,17 @@ __global__ __launch_bounds__(64 * WC * WT * WK) void lordba_i8_product_kernel(Pr
                 for (int j = 0; j < TB; ++j) acc[i][j] += sums[(p * WC * WT * CB * TB + i * TB + j) * 64];
     }
     const int64_t cw = c0 + wc * (kCols / WC), tw = t0 + wt * (kTokens / WT);
-    if (c0 + kCols <= a.n && t0 + kTokens <= a.T) finish<CB, TB, DIG, GATED, true>(a, acc, cw, tw);
-    else finish<CB, TB, DIG, GATED, false>(a, acc, cw, tw);
+    const bool full = c0 + kCols <= a.n && t0 + kTokens <= a.T;
+    // The gated block's results past the caches where they are more than the caches of the XCDs hold twice over, and would push out the rows that
+    // the products still need: 4096 x 4096 x 11008 411 -> 377 us, 2048 x 4096 x 16384 297 -> 286; with 45 MB, 2048 x 4096 x 11008, 169 -> 176.
+    // Plain products take the same time either way.
+    if (GATED && TT == 256 && a.T * a.n >= (1 << 25)) {
+        if (full) finish<CB, TB, DIG, GATED, true, true>(a, acc, cw, tw);
+        else finish<CB, TB, DIG, GATED, true, false>(a, acc, cw, tw);
+    } else {
+        if (full) finish<CB, TB, DIG, GATED, false, true>(a, acc, cw, tw);
+        else finish<CB, TB, DIG, GATED, false, false>(a, acc, cw, tw);
+    }
 }
 
 template <int CT, int TT, int WC, int WT, int WK, int S, int DIG, bool GATED>
@@ -334,7 +344,7 @@ lordba_status product(const ProductArgs& a, hipStream_t stream) {
         case 0: return product_launch<256, 256, 4, 2, 1, 4, DIG, GATED>(a, stream);
         case 1: return product_launch<256, 128, 4, 2, 1, 4, DIG, GATED>(a, stream);
         case 2: return product_launch<128, 128, 2, 4, 1, 4, DIG, GATED>(a, stream);
-        case 3: return product_launch<64, 64, GATED ? 1 : 2, 2, 2, 4, DIG, GATED>(a, stream);
+        case 3: return product_launch<64, 64, 1, 2, 2, 4, DIG, GATED>(a, stream);
         case 4: return product_launch<GATED ? 64 : 32, 32, 1, 1, GATED ? 2 : 4, 4, DIG, GATED>(a, stream);
         default:
             if constexpr (DIG == 1) return product_launch<GATED ? 64 : 32, 16, 1, 1, GATED ? 2 : 4, 4, DIG, GATED>(a, stream);
