@@ -63,8 +63,9 @@ __device__ __forceinline__ void store8(_Float16* row, int64_t c, int64_t n, cons
 // The sums of a lane (CB x TB blocks) to y.  c0, t0: the first column of y and the first token of the wave's part.  A lane has eight
 // consecutive columns of a token in a pair of weight blocks (of gate and of up each), see weight_row.  FULL: all columns and tokens exist.
 // STREAM: the results go past the caches.
-template <int CB, int TB, int DIG, bool GATED, bool STREAM, bool FULL>
-__device__ __forceinline__ void finish(const ProductArgs& a, const i4 (&acc)[CB][TB], int64_t c0, int64_t t0) {
+// addend(p, j, k) gives the lane's eight addends of plane p for its token of block j and its columns of group k.
+template <int CB, int TB, int DIG, bool GATED, bool STREAM, bool FULL, class F>
+__device__ __forceinline__ void finish(const ProductArgs& a, const i4 (&acc)[CB][TB], int64_t c0, int64_t t0, F addend) {
     constexpr int P = GATED ? 2 : 1, G = 2 * P, J = TB / DIG;
     static_assert(CB % G == 0 && TB % DIG == 0, "whole groups of blocks");
     const int lane = threadIdx.x & 63;
@@ -93,7 +94,7 @@ __device__ __forceinline__ void finish(const ProductArgs& a, const i4 (&acc)[CB]
                     for (int p = 0; p < P; ++p)
 #pragma unroll
                         for (int i = 0; i < A; ++i)
-                            add[p][i] = a.addends && (FULL || t + 16 * i < a.T) ? load8<FULL>(a.addends + p * plane + (t + 16 * i) * a.n, c, a.n) : u4{0u, 0u, 0u, 0u};
+                            add[p][i] = addend(p, j + i, cb / G);
                 }
             if (!FULL && t >= a.T) continue;
             float v[P][8];
@@ -206,6 +207,24 @@ __global__ __launch_bounds__(64 * WC * WT * WK) void lordba_i8_product_kernel(Pr
 #pragma unroll
             for (int j = 0; j < TB; ++j) acc[i][j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(fc[set.value][i], ft[set.value][j], acc[i][j], 0, 0, 0);
     };
+    // The addends of a whole tile come the way of the operands: in the last S steps, when there is nothing left to request for the products, each lane
+    // requests those that it will add itself (P planes, TB / DIG tokens, kN groups of columns, eight at a time) into its wave's share of the slots that fall
+    // free.  The products hide what the loads wait for: ADD_FIGURES
+    constexpr int P = GATED ? 2 : 1, kN = CB / (2 * P), kAddends = P * (TB / DIG) * kN;
+    constexpr bool kAhead = GATED && WK == 1 && kAddends <= L * S;
+    const int64_t cw = c0 + wc * (kCols / WC), tw = t0 + wt * (kTokens / WT);
+    const bool full = c0 + kCols <= a.n && t0 + kTokens <= a.T;
+    const bool ahead = kAhead && full && a.addends && K >= S && a.n % 8 == 0 && (reinterpret_cast<uintptr_t>(a.addends) & 15) == 0;
+    const _Float16* const mine = a.addends + (tw + (lane & 15)) * a.n + cw + 8 * (lane >> 4);
+    auto addend_at = [&](int p, int j, int kn) { return mine + (p * a.T + 16 * j) * a.n + 32 * kn; };
+    auto request_addends = [&](int part) {
+#pragma unroll
+        for (int j = 0; j < L; ++j) {   // (always L loads: the waits count on it)
+            const int item = min(part * L + j, kAddends - 1);
+            load16_to_lds<true>(to + j * 1024u, addend_at(item % P, item / P % (TB / DIG), item / (P * (TB / DIG))));
+        }
+        to = to + kSlot == to_end ? to_end - S * kSlot : to + kSlot;
+    };
     // Of this wave's loads all but the youngest LATER steps' have landed, and its operands are in registers; then everybody's.  (The builtin, because
     // the compiler counts the reads of LDS along with it; it does not see the loads.)
     auto meet = [&](auto later) {
@@ -253,12 +272,16 @@ __global__ __launch_bounds__(64 * WC * WT * WK) void lordba_i8_product_kernel(Pr
         using This = std::integral_constant<int, n & 1>;
         using Next = std::integral_constant<int, 1 - (n & 1)>;
         if (k + n + 1 < K) {
-            const int behind = K - 2 - (k + n);
+            const int behind = ahead ? S : K - 2 - (k + n);
             if (behind >= S - 2) meet(Ring{});
             else if (S > 3 && behind == 1) meet(N1{});
             else meet(N0{});
             if (k + n + S < K) request();
+            else if (ahead) request_addends(k + n + S - K);
             read(Next{});
+        } else if (ahead) {   // (everybody has the last step's operands)
+            meet(Ring{});
+            request_addends(S - 1);
         }
         multiply(This{});
         if constexpr (n < S)
@@ -283,18 +306,35 @@ __global__ __launch_bounds__(64 * WC * WT * WK) void lordba_i8_product_kernel(Pr
 #pragma unroll
                 for (int j = 0; j < TB; ++j) acc[i][j] += sums[(p * WC * WT * CB * TB + i * TB + j) * 64];
     }
-    const int64_t cw = c0 + wc * (kCols / WC), tw = t0 + wt * (kTokens / WT);
-    const bool full = c0 + kCols <= a.n && t0 + kTokens <= a.T;
     // The gated block's results past the caches where they are more than the caches of the XCDs hold twice over, and would push out the rows that
     // the products still need: 4096 x 4096 x 11008 411 -> 377 us, 2048 x 4096 x 16384 297 -> 286; with 45 MB, 2048 x 4096 x 11008, 169 -> 176.
     // Plain products take the same time either way.
-    if (GATED && TT == 256 && a.T * a.n >= (1 << 25)) {
-        if (full) finish<CB, TB, DIG, GATED, true, true>(a, acc, cw, tw);
-        else finish<CB, TB, DIG, GATED, true, false>(a, acc, cw, tw);
-    } else {
-        if (full) finish<CB, TB, DIG, GATED, false, true>(a, acc, cw, tw);
-        else finish<CB, TB, DIG, GATED, false, false>(a, acc, cw, tw);
+    auto finish_tile = [&](auto addend) {
+        if (GATED && TT == 256 && a.T * a.n >= (1 << 25)) {
+            if (full) finish<CB, TB, DIG, GATED, true, true>(a, acc, cw, tw, addend);
+            else finish<CB, TB, DIG, GATED, true, false>(a, acc, cw, tw, addend);
+        } else {
+            if (full) finish<CB, TB, DIG, GATED, false, true>(a, acc, cw, tw, addend);
+            else finish<CB, TB, DIG, GATED, false, false>(a, acc, cw, tw, addend);
+        }
+    };
+    auto from_memory = [&](int p, int j, int kn) {
+        const int64_t t = tw + (lane & 15) + 16 * j, c = cw + 8 * (lane >> 4) + 32 * kn;
+        return a.addends && t < a.T ? load_part(a.addends + (p * a.T + t) * a.n, c, a.n) : u4{0u, 0u, 0u, 0u};
+    };
+    if constexpr (kAhead) {
+        if (ahead) {
+            asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+            auto from_lds = [&](int p, int j, int kn) {   // (part 0 lies where the next would go)
+                const int item = p + P * (j + TB / DIG * kn);
+                const uint32_t at = to + item / L * kSlot;
+                return *reinterpret_cast<const u4*>(lds + ((at >= to_end ? at - S * kSlot : at) - base) + item % L * 1024u + lane * 16u);
+            };
+            finish_tile(from_lds);
+            return;
+        }
     }
+    finish_tile(from_memory);
 }
 
 template <int CT, int TT, int WC, int WT, int WK, int S, int DIG, bool GATED>
