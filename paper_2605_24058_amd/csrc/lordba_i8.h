@@ -46,6 +46,46 @@ __device__ __forceinline__ u4 load_part(const _Float16* row, int64_t c, int64_t 
     return v;
 }
 
+constexpr uint32_t kInfBits = 0x7F800000u;
+
+struct RowScale {
+    float inverse, scale;
+};
+// D / amax and amax / D, both correctly rounded; zeros and rows without a number as above.
+__device__ __forceinline__ RowScale scale_of(uint32_t max_bits, float D) {
+    const float amax = __uint_as_float(max_bits);
+    if (max_bits >= kInfBits) return {0.f, __uint_as_float(0x7FC00000u)};
+    if (amax < 0x1p-100f) return {0.f, 0.f};
+    return {D / amax, amax / D};
+}
+
+// Eight numbers into their digits: bytes 0..7 of (hi, lo); with one digit all of it in hi.  Adding 1.5 * 2^23 rounds to an integer (ties to even) and
+// leaves it in two's complement in the low bits of the sum; a byte permutation gathers the bytes of four sums.
+template <int DIG>
+__device__ __forceinline__ void digits_of(const float (&v)[8], float inverse, uint2& hi, uint2& lo) {
+    uint32_t b[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        float q = v[e] * inverse;
+        asm("" : "+v"(q));   // (two roundings, as the definition has it: not one fused operation)
+        b[e] = __float_as_uint(q + 12582912.f);
+    }
+    auto gather = [](uint32_t b0, uint32_t b1, uint32_t b2, uint32_t b3, uint32_t pair) {   // byte `pair & 0xFF` of each
+        return __builtin_amdgcn_perm(__builtin_amdgcn_perm(b3, b2, pair), __builtin_amdgcn_perm(b1, b0, pair), 0x05040100u);
+    };
+    const bool none = inverse == 0.f;   // (a row of zeros, or without a number: infinity times zero is no zero)
+    if constexpr (DIG == 1) {
+        hi = make_uint2(gather(b[0], b[1], b[2], b[3], 0x0400u), gather(b[4], b[5], b[6], b[7], 0x0400u));
+    } else {
+        lo = make_uint2(gather(b[0], b[1], b[2], b[3], 0x0400u), gather(b[4], b[5], b[6], b[7], 0x0400u));
+#pragma unroll
+        for (int e = 0; e < 8; ++e) b[e] += 128;
+        hi = make_uint2(gather(b[0], b[1], b[2], b[3], 0x0501u), gather(b[4], b[5], b[6], b[7], 0x0501u));
+        lo = none ? make_uint2(0, 0) : lo;
+    }
+    hi = none ? make_uint2(0, 0) : hi;
+}
+
 inline lordba_status i8_launched() { return hipGetLastError() == hipSuccess ? LORDBA_OK : LORDBA_ERR_LAUNCH; }
 
 }  // namespace

@@ -24,6 +24,8 @@ struct ProductArgs {
     _Float16* y;              // [T, n]
     _Float16* kept;           // gated: [2, T, n], or null
     int64_t T, n, ld;
+    const _Float16* x;        // OWN_ROWS: [T, d_in], in place of q and q_scale
+    int64_t d_in;
 };
 
 typedef float f4_any __attribute__((ext_vector_type(4), aligned(4)));
@@ -147,6 +149,72 @@ __device__ __forceinline__ Tile tile_of(uint32_t id, uint32_t nc, uint32_t nt) {
     return {in / size, g * kGroup + in % size};
 }
 
+// A few tokens' rows brought to digits by the workgroup itself (OWN_ROWS): x comes into LDS the way of the weights, ahead of them, and its 8-bit rows are
+// kept there.  Behind the ring: x, rows of whole KiB; the rows, a.ld bytes each; their scales.
+__host__ __device__ __forceinline__ int64_t own_x_bytes(int64_t d_in) { return (d_in * 2 + 1023) / 1024 * 1024; }
+__host__ __device__ __forceinline__ int64_t own_bytes(int64_t T, int64_t d_in, int64_t ld) { return T * (own_x_bytes(d_in) + ld) + 64 * 4 * 2; }
+__device__ __forceinline__ int8_t* own_rows_at(const ProductArgs& a, int8_t* lds) { return lds + a.T * own_x_bytes(a.d_in); }
+__device__ __forceinline__ float* own_scales_at(const ProductArgs& a, int8_t* lds) { return reinterpret_cast<float*>(own_rows_at(a, lds) + a.T * a.ld); }
+
+template <int THREADS>
+__device__ __forceinline__ void own_rows_request(const ProductArgs& a, int8_t* lds) {
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+    const uint32_t base = static_cast<uint32_t>(reinterpret_cast<uintptr_t>(lds)), per = static_cast<uint32_t>(own_x_bytes(a.d_in) / 1024);
+    const uint32_t last = static_cast<uint32_t>(a.d_in * 2) - 16;   // (whole 16-byte pieces: d_in is a multiple of 8)
+    for (uint32_t k = wave; k < per * static_cast<uint32_t>(a.T); k += THREADS / 64) {
+        const uint32_t t = k / per, at = min(k % per * 1024u + lane * 16u, last);
+        load16_to_lds<false>(base + k * 1024u, reinterpret_cast<const int8_t*>(a.x + t * a.d_in) + at);
+    }
+}
+
+// LATER: loads that this wave has requested since
+template <int THREADS, int LATER>
+__device__ __forceinline__ void own_rows(const ProductArgs& a, int8_t* lds) {
+    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+    int8_t* const rows = own_rows_at(a, lds);
+    float* const scales = own_scales_at(a, lds);
+    uint32_t* const part = reinterpret_cast<uint32_t*>(scales + 16);   // [token][wave]
+    asm volatile("s_waitcnt vmcnt(%0)" :: "n"(LATER) : "memory");
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+    const uint32_t groups = static_cast<uint32_t>(a.d_in / 8), all = static_cast<uint32_t>(a.ld / 8);
+    for (int t = 0; t < a.T; ++t) {
+        const u4* const x = reinterpret_cast<const u4*>(lds + t * own_x_bytes(a.d_in));
+        uint32_t m = 0;   // (fp16 magnitudes as unsigned numbers, a NaN the largest)
+        for (uint32_t k = threadIdx.x; k < groups; k += THREADS) {
+            const u4 v = x[k];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) m = max(m, max(v[e] & 0x7FFFu, v[e] >> 16 & 0x7FFFu));
+        }
+#pragma unroll
+        for (int s = 32; s > 0; s >>= 1) m = max(m, static_cast<uint32_t>(__shfl_xor(static_cast<int>(m), s)));
+        if (lane == 0) part[t * (THREADS / 64) + wave] = m;
+    }
+    __builtin_amdgcn_s_waitcnt(0xC07F);   // (LDS only: the weights stay on their way)
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+    for (int t = 0; t < a.T; ++t) {
+        const u4* const x = reinterpret_cast<const u4*>(lds + t * own_x_bytes(a.d_in));
+        uint32_t m = part[t * (THREADS / 64)];
+#pragma unroll
+        for (int w = 1; w < THREADS / 64; ++w) m = max(m, part[t * (THREADS / 64) + w]);
+        const RowScale s = scale_of(__float_as_uint(static_cast<float>(__builtin_bit_cast(_Float16, static_cast<uint16_t>(m)))), 127.f);
+        if (threadIdx.x == 0) scales[t] = s.scale;
+        for (uint32_t k = threadIdx.x; k < all; k += THREADS) {
+            const h8 h = as_h8(k < groups ? x[k] : u4{0u, 0u, 0u, 0u});
+            float f[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) f[e] = static_cast<float>(h[e]);
+            uint2 q, none;
+            digits_of<1>(f, s.inverse, q, none);
+            *reinterpret_cast<uint2*>(rows + t * a.ld + 8 * k) = q;
+        }
+    }
+    __builtin_amdgcn_s_waitcnt(0xC07F);
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+}
+
 // One workgroup: CT x TT sums (weight rows x token rows) by WC x WT waves; with WK > 1 as many of those side by side, each with its own 64 columns of a
 // step (short steps wait for their barrier and for LDS, not for data: few tiles want long ones).  A ring of S slots in LDS holds the steps; the loads
 // go straight into it, several steps ahead.
@@ -155,9 +223,9 @@ __device__ __forceinline__ Tile tile_of(uint32_t id, uint32_t nc, uint32_t nt) {
 // the lane, so it is the lane's address that is permuted.
 // While a step's products run on one set of operand registers, the next step's operands are read into the other.
 // The barrier of step k says that step k + 1 has landed and that everybody has read step k, whose slot then takes step k + S.
-template <int CT, int TT, int WC, int WT, int WK, int S, int DIG, bool GATED>
+template <int CT, int TT, int WC, int WT, int WK, int S, int DIG, bool GATED, bool OWN_ROWS = false>
 __global__ __launch_bounds__(64 * WC * WT * WK) void lordba_i8_product_kernel(ProductArgs a) {
-    constexpr int NW = WC * WT * WK, CB = CT / 16 / WC, TB = TT / 16 / WT, NB = (CT + TT) / 16, L = NB * WK / NW;
+    constexpr int NW = WC * WT * WK, CB = CT / 16 / WC, TB = TT / 16 / WT, NB = (OWN_ROWS ? CT : CT + TT) / 16, L = NB * WK / NW;
     constexpr uint32_t kPart = NB * 1024u, kSlot = WK * kPart;
     static_assert(NB * WK % NW == 0 && (S == 3 || S == 4), "whole loads per wave; the waits at the end");
     extern __shared__ int8_t lds[];
@@ -185,6 +253,20 @@ __global__ __launch_bounds__(64 * WC * WT * WK) void lordba_i8_product_kernel(Pr
         }
         to = to + kSlot == to_end ? to_end - S * kSlot : to + kSlot;
     };
+    if constexpr (OWN_ROWS) {
+        static_assert(DIG == 1 && TT == 16 && WC == 1 && WT == 1, "one block of tokens, read by every wave");
+        own_rows_request<64 * NW>(a, lds + S * kSlot);
+    }
+#pragma unroll
+    for (int k = 0; k < S; ++k)
+        if (k < K) request();
+    const int8_t* own = nullptr;
+    if constexpr (OWN_ROWS) {
+        if (K >= S) own_rows<64 * NW, S * L>(a, lds + S * kSlot);
+        else own_rows<64 * NW, 0>(a, lds + S * kSlot);
+        own = own_rows_at(a, lds + S * kSlot) + min<int64_t>(lane & 15, a.T - 1) * a.ld + 64 * wk + 16 * (lane >> 4);
+        a.q_scale = own_scales_at(a, lds + S * kSlot);
+    }
     i4 acc[CB][TB];
 #pragma unroll
     for (int i = 0; i < CB; ++i)
@@ -197,8 +279,14 @@ __global__ __launch_bounds__(64 * WC * WT * WK) void lordba_i8_product_kernel(Pr
     auto read = [&](auto set) {
 #pragma unroll
         for (int i = 0; i < CB; ++i) fc[set.value][i] = *reinterpret_cast<const i4*>(at_c + from + i * 1024);
+        if constexpr (OWN_ROWS) {
+            ft[set.value][0] = *reinterpret_cast<const i4*>(own);
+            if ((lane & 15) >= a.T) ft[set.value][0] = i4{0, 0, 0, 0};
+            own += 64 * WK;
+        } else {
 #pragma unroll
-        for (int i = 0; i < TB; ++i) ft[set.value][i] = *reinterpret_cast<const i4*>(at_t + from + i * 1024);
+            for (int i = 0; i < TB; ++i) ft[set.value][i] = *reinterpret_cast<const i4*>(at_t + from + i * 1024);
+        }
         from = from + kSlot == S * kSlot ? 0 : from + kSlot;
     };
     auto multiply = [&](auto set) {
@@ -247,9 +335,6 @@ __global__ __launch_bounds__(64 * WC * WT * WK) void lordba_i8_product_kernel(Pr
     using N0 = std::integral_constant<int, 0>;
     using N1 = std::integral_constant<int, 1>;
     using Ring = std::integral_constant<int, S - 2>;
-#pragma unroll
-    for (int k = 0; k < S; ++k)
-        if (k < K) request();
     if (K >= S) meet(Ring{});
     else meet(N0{});
     read(N0{});
@@ -337,14 +422,17 @@ __global__ __launch_bounds__(64 * WC * WT * WK) void lordba_i8_product_kernel(Pr
     finish_tile(from_memory);
 }
 
-template <int CT, int TT, int WC, int WT, int WK, int S, int DIG, bool GATED>
+constexpr size_t kLdsBytes = 160 * 1024;
+
+template <int CT, int TT, int WC, int WT, int WK, int S, int DIG, bool GATED, bool OWN_ROWS = false>
 lordba_status product_launch(const ProductArgs& a, hipStream_t stream) {
     constexpr int kCols = GATED ? CT / 2 : CT, kTokens = TT / DIG;
-    constexpr size_t kLds = S * WK * (CT + TT) * 64;
-    static_assert(kLds <= 160 * 1024, "LDS of a compute unit");
-    if constexpr (kLds > 64 * 1024) {
-        if (hipFuncSetAttribute(reinterpret_cast<const void*>(lordba_i8_product_kernel<CT, TT, WC, WT, WK, S, DIG, GATED>),
-                                hipFuncAttributeMaxDynamicSharedMemorySize, kLds) != hipSuccess) {
+    constexpr size_t kRing = S * WK * (OWN_ROWS ? CT : CT + TT) * 64;
+    const size_t lds = kRing + (OWN_ROWS ? static_cast<size_t>(own_bytes(a.T, a.d_in, a.ld)) : 0);
+    static_assert(kRing <= kLdsBytes, "LDS of a compute unit");
+    if (OWN_ROWS || kRing > 64 * 1024) {
+        if (hipFuncSetAttribute(reinterpret_cast<const void*>(lordba_i8_product_kernel<CT, TT, WC, WT, WK, S, DIG, GATED, OWN_ROWS>),
+                                hipFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(OWN_ROWS ? kLdsBytes : kRing)) != hipSuccess) {
             (void)hipGetLastError();
             return LORDBA_ERR_LAUNCH;
         }
@@ -352,7 +440,7 @@ lordba_status product_launch(const ProductArgs& a, hipStream_t stream) {
     const int64_t tiles = (a.n + kCols - 1) / kCols * ((a.T + kTokens - 1) / kTokens);
     if (tiles > INT32_MAX) return LORDBA_ERR_DIM;
     const dim3 grid(static_cast<unsigned>(tiles));
-    hipLaunchKernelGGL((lordba_i8_product_kernel<CT, TT, WC, WT, WK, S, DIG, GATED>), grid, dim3(64 * WC * WT * WK), kLds, stream, a);
+    hipLaunchKernelGGL((lordba_i8_product_kernel<CT, TT, WC, WT, WK, S, DIG, GATED, OWN_ROWS>), grid, dim3(64 * WC * WT * WK), lds, stream, a);
     return i8_launched();
 }
 
@@ -390,6 +478,16 @@ lordba_status product(const ProductArgs& a, hipStream_t stream) {
             if constexpr (DIG == 1) return product_launch<GATED ? 64 : 32, 16, 1, 1, GATED ? 2 : 4, 4, DIG, GATED>(a, stream);
             return LORDBA_ERR_LAUNCH;   // (cheapest_tile does not name it)
     }
+}
+
+// Whether the product's workgroups bring the rows to digits themselves: one launch instead of two, but every workgroup does the whole of it.  Times of a
+// call in us, with the row kernel -> without, T x d_in -> d_out: 1 x 4096 -> 4096 7.9 -> 5.8, 1 x 4096 -> 11008 12.2 -> 8.9, 1 x 11008 -> 4096 13.2 -> 11.7,
+// 2 x 4096 -> 4096 8.0 -> 6.8, 2 x 11008 -> 4096 13.1 -> 13.6, 4 x 1000 -> 1024 8.2 -> 5.9, 4 x 4096 -> 11008 12.4 -> 17.8; gated, 1 x 4096 x 11008
+// 19.6 -> 17.2, 2 x 4096 x 11008 19.4 -> 21.9.
+template <bool GATED>
+bool own_rows_fit(const ProductArgs& a, int digits) {
+    return digits == 1 && a.T <= 16 && a.T * a.d_in <= (GATED ? 6144 : 14336) && a.d_in % 8 == 0 && !i8_misaligned(a.x, 16) &&
+           static_cast<size_t>(own_bytes(a.T, a.d_in, a.ld)) + 4 * 4 * (GATED ? 64 : 32) * 64 <= kLdsBytes;
 }
 
 // What the four entry points check alike.
@@ -439,9 +537,11 @@ lordba_status linear(const void* x, const float* col_scale, const int8_t* w, con
     if (dev != LORDBA_OK) return dev;
     const hipStream_t st = static_cast<hipStream_t>(stream);
     const Workspace ws = split(workspace, T, contracted, digits);
+    const ProductArgs a = {w, ws.q, ws.scale, w_scale, nullptr, static_cast<_Float16*>(y), nullptr, T, n, i8_row_bytes(contracted),
+                           static_cast<const _Float16*>(x), contracted};
+    if (!col_scale && own_rows_fit<false>(a, digits)) return product_launch<32, 16, 1, 1, 4, 4, 1, false, true>(a, st);
     const lordba_status rows = lordba_i8_quantize(x, col_scale, ws.q, ws.scale, T, contracted, digits, st);
     if (rows != LORDBA_OK) return rows;
-    const ProductArgs a = {w, ws.q, ws.scale, w_scale, nullptr, static_cast<_Float16*>(y), nullptr, T, n, i8_row_bytes(contracted)};
     return digits == 1 ? product<1, false>(a, st) : product<2, false>(a, st);
 }
 
@@ -478,9 +578,10 @@ extern "C" lordba_status lordba_gated_i8(const void* x, const int8_t* W, const f
     if ((st = check_device()) != LORDBA_OK) return st;
     const hipStream_t s = static_cast<hipStream_t>(stream);
     const Workspace ws = split(workspace, T, d_in, digits);
-    if ((st = lordba_i8_quantize(x, nullptr, ws.q, ws.scale, T, d_in, digits, s)) != LORDBA_OK) return st;
     const ProductArgs a = {W, ws.q, ws.scale, w_scale, static_cast<const _Float16*>(addends), static_cast<_Float16*>(h), static_cast<_Float16*>(gate_up),
-                           T, d_ff, i8_row_bytes(d_in)};
+                           T, d_ff, i8_row_bytes(d_in), static_cast<const _Float16*>(x), d_in};
+    if (own_rows_fit<true>(a, digits)) return product_launch<64, 16, 1, 1, 4, 4, 1, true, true>(a, s);
+    if ((st = lordba_i8_quantize(x, nullptr, ws.q, ws.scale, T, d_in, digits, s)) != LORDBA_OK) return st;
     return digits == 1 ? product<1, true>(a, s) : product<2, true>(a, s);
 }
 
@@ -502,6 +603,6 @@ extern "C" lordba_status lordba_gated_i8_backward(const void* dh, const void* ga
     const hipStream_t s = static_cast<hipStream_t>(stream);
     const Workspace ws = split(workspace, T, 2 * d_ff, digits);
     if ((st = lordba_i8_gated_grad(dh, gate_up, w_scale, dgate_up, ws.q, ws.scale, T, d_ff, digits, s)) != LORDBA_OK) return st;
-    const ProductArgs a = {Wt, ws.q, ws.scale, nullptr, nullptr, static_cast<_Float16*>(dx), nullptr, T, d_in, i8_row_bytes(2 * d_ff)};
+    const ProductArgs a = {Wt, ws.q, ws.scale, nullptr, nullptr, static_cast<_Float16*>(dx), nullptr, T, d_in, i8_row_bytes(2 * d_ff), nullptr, 0};
     return digits == 1 ? product<1, false>(a, s) : product<2, false>(a, s);
 }
