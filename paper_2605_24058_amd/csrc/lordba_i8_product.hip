@@ -46,12 +46,15 @@ __device__ __forceinline__ void load8(const float* p, int64_t c, int64_t n, floa
         for (int e = 0; e < 8; ++e) v[e] = p[min(c + e, n - 1)];
     }
 }
-template <bool FULL, bool STREAM = false>
-__device__ __forceinline__ void store8(_Float16* row, int64_t c, int64_t n, const float (&f)[8]) {
+__device__ __forceinline__ u4 to_halves(const float (&f)[8]) {
     h8 h;
 #pragma unroll
     for (int e = 0; e < 8; ++e) h[e] = static_cast<_Float16>(f[e]);
-    const u4 v = __builtin_bit_cast(u4, h);
+    return __builtin_bit_cast(u4, h);
+}
+template <bool FULL, bool STREAM = false>
+__device__ __forceinline__ void store8(_Float16* row, int64_t c, int64_t n, const float (&f)[8]) {
+    const u4 v = to_halves(f);
     if (FULL || c + 8 <= n) {
         if constexpr (STREAM) store16_any_stream(row + c, v);
         else *reinterpret_cast<u4_any*>(row + c) = v;
@@ -61,12 +64,34 @@ __device__ __forceinline__ void store8(_Float16* row, int64_t c, int64_t n, cons
             if (c + e < n) reinterpret_cast<uint16_t*>(row)[c + e] = static_cast<uint16_t>(v[e >> 1] >> (16 * (e & 1)));
     }
 }
+// The same for rows of which every other one starts in the middle of a word (an odd n), all lanes here: the four lane groups' 32 columns are stored
+// from their second column on, one further for each lane, so that the wide stores start on words (the memory path takes stores that do not apart).
+// 4096 x 8191 results 48 us -> 39 with 128 x 128 tiles, 50 -> 45 with 256 x 256.
+__device__ __forceinline__ void store8_odd(_Float16* p, const float (&f)[8]) {
+    typedef uint32_t u3_word __attribute__((ext_vector_type(3), aligned(4)));
+    const u4 v = to_halves(f);
+    const int g = (threadIdx.x & 63) >> 4;
+    const bool odd = (reinterpret_cast<uintptr_t>(p) & 2) != 0;
+    const uint32_t next = static_cast<uint32_t>(__shfl_down(static_cast<int>(v[0]), 16));
+    const u4 moved = {__builtin_amdgcn_alignbit(v[1], v[0], 16), __builtin_amdgcn_alignbit(v[2], v[1], 16), __builtin_amdgcn_alignbit(v[3], v[2], 16),
+                      __builtin_amdgcn_alignbit(next, v[3], 16)};
+    uint16_t* const h = reinterpret_cast<uint16_t*>(p);
+    if (!odd || g < 3) {
+        u4_word* const to = reinterpret_cast<u4_word*>(h + odd);
+        *to = odd ? moved : v;
+    } else {
+        *reinterpret_cast<u3_word*>(h + 1) = u3_word{moved[0], moved[1], moved[2]};
+        h[7] = static_cast<uint16_t>(v[3] >> 16);
+    }
+    if (odd && g == 0) h[0] = static_cast<uint16_t>(v[0]);
+}
 
 // The sums of a lane (CB x TB blocks) to y.  c0, t0: the first column of y and the first token of the wave's part.  A lane has eight
 // consecutive columns of a token in a pair of weight blocks (of gate and of up each), see weight_row.  FULL: all columns and tokens exist.
-// STREAM: the results go past the caches.
+// ODD: n is odd, or y starts in the middle of a word.  LINES: every piece of 32 columns
+// is 64 aligned bytes; what is kept then goes past the caches, with STREAM y too.
 // addend(p, j, k) gives the lane's eight addends of plane p for its token of block j and its columns of group k.
-template <int CB, int TB, int DIG, bool GATED, bool STREAM, bool FULL, class F>
+template <int CB, int TB, int DIG, bool GATED, bool FULL, bool ODD, bool LINES, bool STREAM, class F>
 __device__ __forceinline__ void finish(const ProductArgs& a, const i4 (&acc)[CB][TB], int64_t c0, int64_t t0, F addend) {
     constexpr int P = GATED ? 2 : 1, G = 2 * P, J = TB / DIG;
     static_assert(CB % G == 0 && TB % DIG == 0, "whole groups of blocks");
@@ -111,14 +136,18 @@ __device__ __forceinline__ void finish(const ProductArgs& a, const i4 (&acc)[CB]
                     if constexpr (GATED) v[p][e] += static_cast<float>(as_h8(add[p][j % A])[e]);
                 }
             if constexpr (GATED) {
-                if (a.kept) {   // (wanted by the backward pass only: past the caches, which the products' rows need; 189 -> 178 us at 2048 x 4096 x 11008)
-                    store8<FULL, true>(a.kept + t * a.n, c, a.n, v[0]);
-                    store8<FULL, true>(a.kept + plane + t * a.n, c, a.n, v[1]);
+                if (a.kept && ODD) {
+                    store8_odd(a.kept + t * a.n + c, v[0]);
+                    store8_odd(a.kept + plane + t * a.n + c, v[1]);
+                } else if (a.kept) {
+                    store8<FULL, LINES>(a.kept + t * a.n, c, a.n, v[0]);
+                    store8<FULL, LINES>(a.kept + plane + t * a.n, c, a.n, v[1]);
                 }
 #pragma unroll
                 for (int e = 0; e < 8; ++e) v[0][e] = v[0][e] * __builtin_amdgcn_rcpf(1.f + __expf(-v[0][e])) * v[1][e];
             }
-            store8<FULL, STREAM>(a.y + t * a.n, c, a.n, v[0]);
+            if constexpr (ODD) store8_odd(a.y + t * a.n + c, v[0]);
+            else store8<FULL, STREAM>(a.y + t * a.n, c, a.n, v[0]);
         }
     }
 }
@@ -391,17 +420,20 @@ __global__ __launch_bounds__(64 * WC * WT * WK) void lordba_i8_product_kernel(Pr
 #pragma unroll
                 for (int j = 0; j < TB; ++j) acc[i][j] += sums[(p * WC * WT * CB * TB + i * TB + j) * 64];
     }
-    // The gated block's results past the caches where they are more than the caches of the XCDs hold twice over, and would push out the rows that
-    // the products still need: 4096 x 4096 x 11008 411 -> 377 us, 2048 x 4096 x 16384 297 -> 286; with 45 MB, 2048 x 4096 x 11008, 169 -> 176.
-    // Plain products take the same time either way.
+    // What only the backward pass wants goes past the caches, which hold rows that the products still need: 512 x 4096 x 11008 60 -> 54 us,
+    // 4096 x 4096 x 11008 386 -> 371, 8192 x 1024 x 8192 262 -> 237; pieces of lines that others finish do not (4096 x 500 x 4088 49 -> 69 if they did).
+    // y too where it is more than the caches of the XCDs hold twice over.  Plain products take the same time either way.
     auto finish_tile = [&](auto addend) {
-        if (GATED && TT == 256 && a.T * a.n >= (1 << 25)) {
-            if (full) finish<CB, TB, DIG, GATED, true, true>(a, acc, cw, tw, addend);
-            else finish<CB, TB, DIG, GATED, true, false>(a, acc, cw, tw, addend);
-        } else {
-            if (full) finish<CB, TB, DIG, GATED, false, true>(a, acc, cw, tw, addend);
-            else finish<CB, TB, DIG, GATED, false, false>(a, acc, cw, tw, addend);
-        }
+        using No = std::false_type;
+        using Yes = std::true_type;
+        auto go = [&](auto whole, auto odd, auto lines, auto stream) {
+            finish<CB, TB, DIG, GATED, whole.value, odd.value, lines.value, stream.value>(a, acc, cw, tw, addend);
+        };
+        if (!full) go(No{}, No{}, No{}, No{});
+        else if ((a.n & 1) || ((reinterpret_cast<uintptr_t>(a.y) | reinterpret_cast<uintptr_t>(a.kept)) & 2)) go(Yes{}, Yes{}, No{}, No{});
+        else if (!GATED || a.n % 32 != 0 || ((reinterpret_cast<uintptr_t>(a.y) | reinterpret_cast<uintptr_t>(a.kept)) & 63) != 0) go(Yes{}, No{}, No{}, No{});
+        else if (TT < 256 || a.T * a.n < (1 << 25)) go(Yes{}, No{}, Yes{}, No{});
+        else go(Yes{}, No{}, Yes{}, Yes{});
     };
     auto from_memory = [&](int p, int j, int kn) {
         const int64_t t = tw + (lane & 15) + 16 * j, c = cw + 8 * (lane >> 4) + 32 * kn;

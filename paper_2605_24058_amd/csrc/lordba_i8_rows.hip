@@ -161,8 +161,11 @@ __device__ __forceinline__ void store_bytes(int8_t* p, uint2 v, int64_t n) {
 
 // NV > 0: a thread's numbers stay in registers; NV = 0 (d_ff > 16384): they are computed again for the second pass
 template <int TPR, int NV, int DIG>
-__global__ __launch_bounds__(TPR) void lordba_gated_grad_kernel(GatedGradArgs a) {
-    const int64_t row = blockIdx.x, F = a.d_ff, plane = a.T * F;
+__global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void lordba_gated_grad_kernel(GatedGradArgs a) {
+    const int tid = threadIdx.x % TPR;
+    const int64_t row = TPR < 256 ? static_cast<int64_t>(blockIdx.x) * (256 / TPR) + threadIdx.x / TPR : blockIdx.x;
+    if (row >= a.T) return;   // (whole waves: a wave has one row)
+    const int64_t F = a.d_ff, plane = a.T * F;
     const _Float16 *dh = a.dh + row * F, *gate = a.gate_up + row * F, *up = gate + plane;
     _Float16 *dgate = a.dgate_up + row * F, *dup = dgate + plane;
     const int turns = NV > 0 ? NV : static_cast<int>((F + 8 * TPR - 1) / (8 * TPR));
@@ -170,7 +173,7 @@ __global__ __launch_bounds__(TPR) void lordba_gated_grad_kernel(GatedGradArgs a)
     uint32_t m = 0;
 #pragma unroll NV > 0 ? NV : 1
     for (int i = 0; i < turns; ++i) {
-        const int64_t c = 8 * static_cast<int64_t>(threadIdx.x + i * TPR);
+        const int64_t c = 8 * static_cast<int64_t>(tid + i * TPR);
         if (c >= F) break;
         float dg[8], du[8];
         gated_grad(as_h8(load_part(dh, c, F)), as_h8(load_part(gate, c, F)), as_h8(load_part(up, c, F)), dg, du);
@@ -194,12 +197,12 @@ __global__ __launch_bounds__(TPR) void lordba_gated_grad_kernel(GatedGradArgs a)
         store_part(dup, c, F, __builtin_bit_cast(u4, hu));
     }
     const RowScale s = scale_of(row_max<TPR>(m), DIG == 1 ? 127.f : 32512.f);
-    if (threadIdx.x == 0) a.scale[row] = s.scale;
+    if (tid == 0) a.scale[row] = s.scale;
     int8_t* const q = a.q + row * a.ld;
     int8_t* const q_lo = q + a.T * a.ld;
 #pragma unroll NV > 0 ? NV : 1
     for (int i = 0; i < turns; ++i) {
-        const int64_t c = 8 * static_cast<int64_t>(threadIdx.x + i * TPR);
+        const int64_t c = 8 * static_cast<int64_t>(tid + i * TPR);
         if (c >= F) break;
         float dg[8], du[8];
         if constexpr (NV > 0) {
@@ -221,7 +224,7 @@ __global__ __launch_bounds__(TPR) void lordba_gated_grad_kernel(GatedGradArgs a)
         store_bytes(q + F + c, hi, F - c);
         if constexpr (DIG == 2) store_bytes(q_lo + F + c, lo, F - c);
     }
-    for (int64_t c = 2 * F + threadIdx.x; c < a.ld; c += TPR) {
+    for (int64_t c = 2 * F + tid; c < a.ld; c += TPR) {
         q[c] = 0;
         if constexpr (DIG == 2) q_lo[c] = 0;
     }
@@ -229,9 +232,12 @@ __global__ __launch_bounds__(TPR) void lordba_gated_grad_kernel(GatedGradArgs a)
 
 template <int DIG>
 lordba_status gated_grad_launch(const GatedGradArgs& a, hipStream_t stream) {
-    const dim3 grid(static_cast<unsigned>(a.T));
-    // (1024 threads of two groups each, for the longest rows, spilled: 72 us instead of 62 at 2048 x 11008)
-    if (a.d_ff <= 2048) hipLaunchKernelGGL((lordba_gated_grad_kernel<256, 1, DIG>), grid, dim3(256), 0, stream, a);
+    const dim3 grid(static_cast<unsigned>(a.T)), waves(static_cast<unsigned>((a.T + 3) / 4));
+    // Up to 1024 columns a wave has a row of its own (16384 x 320: 58 -> 27 us for the call).  (1024 threads of two groups each, for the longest rows, spilled: 72 us instead
+    // of 62 at 2048 x 11008.)
+    if (a.d_ff <= 512) hipLaunchKernelGGL((lordba_gated_grad_kernel<64, 1, DIG>), waves, dim3(256), 0, stream, a);
+    else if (a.d_ff <= 1024) hipLaunchKernelGGL((lordba_gated_grad_kernel<64, 2, DIG>), waves, dim3(256), 0, stream, a);
+    else if (a.d_ff <= 2048) hipLaunchKernelGGL((lordba_gated_grad_kernel<256, 1, DIG>), grid, dim3(256), 0, stream, a);
     else if (a.d_ff <= 4096) hipLaunchKernelGGL((lordba_gated_grad_kernel<512, 1, DIG>), grid, dim3(512), 0, stream, a);
     else if (a.d_ff <= 8192) hipLaunchKernelGGL((lordba_gated_grad_kernel<512, 2, DIG>), grid, dim3(512), 0, stream, a);
     else if (a.d_ff <= 16384) hipLaunchKernelGGL((lordba_gated_grad_kernel<512, 4, DIG>), grid, dim3(512), 0, stream, a);
