@@ -1,6 +1,9 @@
 // Dropout whose mask is a function of the element's index: Philox4x32-10 (J. Salmon et al., "Parallel random numbers: as easy as 1, 2, 3", 2011)
 // with the counter (index / 8, offset) and the seed as the key gives 128 bits for eight elements, 16 for each.  Nothing but the tensor moves: the
 // backward pass draws the same bits again.
+#include <algorithm>
+#include <cmath>
+
 #include "lordba_dev_util.h"
 #include "lordba_i8.h"
 
@@ -13,6 +16,7 @@ struct DropoutArgs {
     const uint64_t* offset_dev;   // or null
     uint64_t seed, offset;
     int64_t n;
+    int64_t first;   // group of eight elements of this launch's first thread
     uint32_t least;   // what is kept has draws from here on: 0 .. 65536
     float factor;
 };
@@ -35,7 +39,7 @@ __device__ __forceinline__ u4 philox(uint64_t group, uint64_t offset, uint64_t s
 
 template <bool BASE>
 __global__ __launch_bounds__(256) void lordba_dropout_kernel(DropoutArgs a) {
-    const int64_t group = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x, i = 8 * group;
+    const int64_t group = a.first + static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x, i = 8 * group;
     if (i >= a.n) return;
     const u4 r = philox(static_cast<uint64_t>(group), a.offset + (a.offset_dev ? *a.offset_dev : 0), a.seed);
     const bool whole = i + 8 <= a.n;
@@ -74,7 +78,7 @@ __global__ __launch_bounds__(256) void lordba_dropout_kernel(DropoutArgs a) {
 
 extern "C" lordba_status lordba_dropout(const void* x, const void* y_base, void* y_out, int64_t n, double p, uint64_t seed, uint64_t offset,
                                         const uint64_t* offset_dev, void* stream) {
-    if (n < 0 || n > (static_cast<int64_t>(1) << 38)) return LORDBA_ERR_DIM;   // (a grid holds 2^31 - 1 workgroups of 2048 elements)
+    if (n < 0 || n > (static_cast<int64_t>(1) << 38)) return LORDBA_ERR_DIM;
     if (!(p >= 0. && p <= 1.)) return LORDBA_ERR_VALUE;
     if (n == 0) return LORDBA_OK;
     if (!x || !y_out) return LORDBA_ERR_NULL;
@@ -86,10 +90,15 @@ extern "C" lordba_status lordba_dropout(const void* x, const void* y_base, void*
     const lordba_status dev = check_device();
     if (dev != LORDBA_OK) return dev;
     const uint32_t least = static_cast<uint32_t>(nearbyint(p * 65536.));
-    const DropoutArgs a = {static_cast<const _Float16*>(x), static_cast<const _Float16*>(y_base), static_cast<_Float16*>(y_out), offset_dev,
-                           seed, offset, n, least, least < 65536 ? 65536.f / static_cast<float>(65536 - least) : 0.f};
-    const dim3 grid(static_cast<unsigned>((n + 2047) / 2048));
-    if (y_base) hipLaunchKernelGGL(lordba_dropout_kernel<true>, grid, dim3(256), 0, static_cast<hipStream_t>(stream), a);
-    else hipLaunchKernelGGL(lordba_dropout_kernel<false>, grid, dim3(256), 0, static_cast<hipStream_t>(stream), a);
-    return i8_launched();
+    DropoutArgs a = {static_cast<const _Float16*>(x), static_cast<const _Float16*>(y_base), static_cast<_Float16*>(y_out), offset_dev,
+                           seed, offset, n, 0, least, least < 65536 ? 65536.f / static_cast<float>(65536 - least) : 0.f};
+    const int64_t groups = (n + 7) / 8, most = static_cast<int64_t>(1) << 31;   // (a launch counts threads in 32 bits)
+    for (a.first = 0; a.first < groups; a.first += most) {
+        const dim3 grid(static_cast<unsigned>((std::min(most, groups - a.first) + 255) / 256));
+        if (y_base) hipLaunchKernelGGL(lordba_dropout_kernel<true>, grid, dim3(256), 0, static_cast<hipStream_t>(stream), a);
+        else hipLaunchKernelGGL(lordba_dropout_kernel<false>, grid, dim3(256), 0, static_cast<hipStream_t>(stream), a);
+        const lordba_status st = i8_launched();
+        if (st != LORDBA_OK) return st;
+    }
+    return LORDBA_OK;
 }

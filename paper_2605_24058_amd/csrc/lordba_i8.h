@@ -27,6 +27,16 @@ inline size_t i8_scale_offset(int64_t T, int64_t cols, int digits) {   // the ro
     return (static_cast<size_t>(digits) * static_cast<size_t>(T) * static_cast<size_t>(i8_row_bytes(cols)) + 255) / 256 * 256;
 }
 
+// Few rows of a long contraction: behind them lies room for the counters and the partial sums of kI8SplitTiles workgroups of 64 x 32 sums.
+constexpr int64_t kI8SplitColumns = 2048, kI8SplitRows = 512, kI8SplitTiles = 256;
+inline bool i8_splits(int64_t T, int64_t cols, int digits) { return i8_row_bytes(cols) >= kI8SplitColumns && T * digits <= kI8SplitRows; }
+inline size_t i8_split_offset(int64_t T, int64_t cols, int digits) {
+    return (i8_scale_offset(T, cols, digits) + static_cast<size_t>(T) * 4 + 255) / 256 * 256;
+}
+inline size_t i8_workspace_bytes(int64_t T, int64_t cols, int digits) {
+    return i8_split_offset(T, cols, digits) + (i8_splits(T, cols, digits) ? kI8SplitTiles * (4 + 64 * 32 * 4) : 0);
+}
+
 inline bool i8_overlap(const void* p, size_t pn, const void* q, size_t qn) {
     const uintptr_t a = reinterpret_cast<uintptr_t>(p), b = reinterpret_cast<uintptr_t>(q);
     return p && q && pn && qn && a < b + qn && b < a + pn;
@@ -91,7 +101,8 @@ inline lordba_status i8_launched() { return hipGetLastError() == hipSuccess ? LO
 }  // namespace
 
 // The steps of the entry points; arguments have been checked.  Each enqueues one kernel.
-lordba_status lordba_i8_quantize(const void* x, const float* col_scale, int8_t* q, float* scale, int64_t rows, int64_t cols, int digits,
-                                 hipStream_t stream);
+// `clear`: kI8SplitTiles words that the kernel sets to zero on its way, or null.
+lordba_status lordba_i8_quantize(const void* x, const float* col_scale, int8_t* q, float* scale, uint32_t* clear, int64_t rows, int64_t cols,
+                                 int digits, hipStream_t stream);
 lordba_status lordba_i8_gated_grad(const void* dh, const void* gate_up, const float* w_scale, void* dgate_up, int8_t* q, float* scale,
-                                   int64_t T, int64_t d_ff, int digits, hipStream_t stream);
+                                   uint32_t* clear, int64_t T, int64_t d_ff, int digits, hipStream_t stream);

@@ -26,6 +26,10 @@ struct ProductArgs {
     int64_t T, n, ld;
     const _Float16* x;        // OWN_ROWS: [T, d_in], in place of q and q_scale
     int64_t d_in;
+    int32_t* parts;           // splits > 1: [splits, tiles, 16 x 16 blocks] sums, behind the tiles' counters of arrivals (zeros)
+    uint32_t* arrived;
+    uint32_t splits;
+    uint32_t first;           // tile of this launch's first workgroup
 };
 
 typedef float f4_any __attribute__((ext_vector_type(4), aligned(4)));
@@ -261,15 +265,19 @@ __global__ __launch_bounds__(64 * WC * WT * WK) void lordba_i8_product_kernel(Pr
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int wc = wave % WC, wt = wave / WC % WT, wk = wave / (WC * WT);
     constexpr int kCols = GATED ? CT / 2 : CT, kTokens = TT / DIG;
-    const Tile tile = tile_of(blockIdx.x, static_cast<uint32_t>((a.n + kCols - 1) / kCols), static_cast<uint32_t>((a.T + kTokens - 1) / kTokens));
+    const Tile tile = tile_of(a.first + blockIdx.x, static_cast<uint32_t>((a.n + kCols - 1) / kCols), static_cast<uint32_t>((a.T + kTokens - 1) / kTokens));
     const int64_t c0 = static_cast<int64_t>(tile.c) * kCols, t0 = static_cast<int64_t>(tile.t) * kTokens;
-    const int K = static_cast<int>(a.ld / (64 * WK));
+    // (SPLIT: this workgroup has the steps k0 .. k0 + K - 1 of the contraction)
+    constexpr bool SPLIT = WC * WT == 1 && WK > 1 && !OWN_ROWS;
+    const int steps = static_cast<int>(a.ld / (64 * WK));
+    const int k0 = SPLIT ? static_cast<int>(static_cast<int64_t>(steps) * blockIdx.y / a.splits) : 0;
+    const int K = SPLIT ? static_cast<int>(static_cast<int64_t>(steps) * (blockIdx.y + 1) / a.splits) - k0 : steps;
 
     const int8_t* src[L];
 #pragma unroll
     for (int j = 0; j < L; ++j) {
         const int b = (wave * L + j) % NB, part = (wave * L + j) / NB, r = lane >> 2, piece = (lane & 3) ^ ((r >> 1) & 3);
-        src[j] = (b < CT / 16 ? weight_row<GATED>(a, c0, b, r) : token_row<DIG>(a, t0, b - CT / 16, r)) + 64 * part + 16 * piece;
+        src[j] = (b < CT / 16 ? weight_row<GATED>(a, c0, b, r) : token_row<DIG>(a, t0, b - CT / 16, r)) + (k0 * WK + part) * 64 + 16 * piece;
     }
     const uint32_t base = static_cast<uint32_t>(reinterpret_cast<uintptr_t>(lds));
     uint32_t to = base + wave * L * 1024u, from = 0;   // the slot that the next step is requested into, and the one that is read next
@@ -420,6 +428,43 @@ __global__ __launch_bounds__(64 * WC * WT * WK) void lordba_i8_product_kernel(Pr
 #pragma unroll
                 for (int j = 0; j < TB; ++j) acc[i][j] += sums[(p * WC * WT * CB * TB + i * TB + j) * 64];
     }
+    if constexpr (SPLIT) {
+        // The last workgroup of a tile to arrive joins the parts: whole numbers, any order gives the same sum.  The parts go through the memory that all XCDs
+        // share, piece by piece (accesses of agent scope), not by a fence, which would have the XCD's whole L2 written back: 49 x 12306 -> 196 20.7 us.
+        if (a.splits > 1) {
+            uint64_t* const parts = reinterpret_cast<uint64_t*>(a.parts) + static_cast<int64_t>(blockIdx.x) * (CB * TB * 128) + lane;
+            const int64_t apart = static_cast<int64_t>(gridDim.x) * (CB * TB * 128);
+            typedef uint64_t l2v __attribute__((ext_vector_type(2)));
+#pragma unroll
+            for (int i = 0; i < CB * TB; ++i) {
+                const l2v v = __builtin_bit_cast(l2v, acc[i / TB][i % TB]);
+#pragma unroll
+                for (int k = 0; k < 2; ++k) __hip_atomic_store(parts + blockIdx.y * apart + i * 128 + k * 64, v[k], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+            }
+            asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // (the parts are there before the arrival is counted)
+            uint32_t before = 0;
+            if (lane == 0) before = __hip_atomic_fetch_add(a.arrived + blockIdx.x, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+            if (__builtin_amdgcn_readfirstlane(before) + 1 != a.splits) return;
+            asm volatile("" ::: "memory");
+            // several parts are on their way at a time: each way takes about a microsecond
+            constexpr uint32_t kTogether = CB * TB > 4 ? 4 : 8;
+            for (uint32_t p0 = 0; p0 < a.splits; p0 += kTogether) {
+                uint64_t v[kTogether][CB * TB][2];
+#pragma unroll
+                for (uint32_t u = 0; u < kTogether; ++u)
+#pragma unroll
+                    for (int i = 0; i < CB * TB; ++i)
+#pragma unroll
+                        for (int k = 0; k < 2; ++k)
+                            v[u][i][k] = __hip_atomic_load(parts + min(p0 + u, a.splits - 1) * apart + i * 128 + k * 64, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+#pragma unroll
+                for (uint32_t u = 0; u < kTogether; ++u)
+                    if (p0 + u < a.splits && p0 + u != blockIdx.y)
+#pragma unroll
+                        for (int i = 0; i < CB * TB; ++i) acc[i / TB][i % TB] += __builtin_bit_cast(i4, l2v{v[u][i][0], v[u][i][1]});
+            }
+        }
+    }
     // What only the backward pass wants goes past the caches, which hold rows that the products still need: 512 x 4096 x 11008 60 -> 54 us,
     // 4096 x 4096 x 11008 386 -> 371, 8192 x 1024 x 8192 262 -> 237; pieces of lines that others finish do not (4096 x 500 x 4088 49 -> 69 if they did).
     // y too where it is more than the caches of the XCDs hold twice over.  Plain products take the same time either way.
@@ -471,36 +516,56 @@ lordba_status product_launch(const ProductArgs& a, hipStream_t stream) {
     }
     const int64_t tiles = (a.n + kCols - 1) / kCols * ((a.T + kTokens - 1) / kTokens);
     if (tiles > INT32_MAX) return LORDBA_ERR_DIM;
-    const dim3 grid(static_cast<unsigned>(tiles));
-    hipLaunchKernelGGL((lordba_i8_product_kernel<CT, TT, WC, WT, WK, S, DIG, GATED, OWN_ROWS>), grid, dim3(64 * WC * WT * WK), lds, stream, a);
-    return i8_launched();
+    constexpr int64_t kMost = (static_cast<int64_t>(1) << 31) / (64 * WC * WT * WK);   // (a launch counts threads in 32 bits)
+    for (int64_t first = 0; first < tiles; first += kMost) {
+        ProductArgs part = a;
+        part.first = static_cast<uint32_t>(first);
+        hipLaunchKernelGGL((lordba_i8_product_kernel<CT, TT, WC, WT, WK, S, DIG, GATED, OWN_ROWS>),
+                           dim3(static_cast<unsigned>(std::min(kMost, tiles - first)), a.splits), dim3(64 * WC * WT * WK), lds, stream, part);
+        const lordba_status st = i8_launched();
+        if (st != LORDBA_OK) return st;
+    }
+    return LORDBA_OK;
 }
 
-// The tiles and what a step of 64 columns of one takes on a compute unit, in nanoseconds: alone on a chip with few workgroups (waiting), and as a
-// share of a chip that is full (throughput; small tiles run side by side on a unit).  Measured on square and ragged shapes of 1 to 16384 rows;
-// the sum below is within 30 % of what a call takes and picks the fastest tile or one within 10 % of it on all of those.
+// The tiles and their times on a compute unit, in nanoseconds: a step of 64 columns alone on a chip with few workgroups (waiting), the same as a share of
+// a chip that is full (throughput; small tiles run side by side on a unit), and the filling and emptying around the steps.
 struct TileCost {
     int channels, tokens;
-    double alone, share;
+    double alone, share, fixed;
 };
-constexpr TileCost kTiles[] = {{256, 256, 600, 800}, {256, 128, 390, 510}, {128, 128, 200, 300}, {64, 64, 77, 125}, {32, 32, 35, 60}, {32, 16, 25, 50}};
-constexpr TileCost kGatedTiles[] = {{256, 256, 600, 800}, {256, 128, 390, 510}, {128, 128, 200, 300}, {64, 64, 77, 125}, {64, 32, 60, 105}, {64, 16, 40, 100}};
+constexpr TileCost kTiles[] = {{256, 256, 600, 800, 7000}, {256, 128, 390, 510, 3400}, {128, 128, 200, 300, 1100}, {64, 64, 77, 125, 600}, {32, 32, 35, 60, 300}, {32, 16, 25, 50, 300}};
+constexpr TileCost kGatedTiles[] = {{256, 256, 600, 800, 7000}, {256, 128, 390, 510, 3400}, {128, 128, 200, 300, 1100}, {64, 64, 77, 125, 600}, {64, 32, 60, 105, 500}, {64, 16, 40, 100, 400}};
 
-int cheapest_tile(const TileCost (&tiles)[6], int64_t channels, int64_t rows, bool two_digits) {
-    int best = 0;
+// Few small tiles of a long contraction: several workgroups share a tile's steps, which costs them kJoin ns to join (24 x 12306 -> 196: SPLIT_FIGURE).
+constexpr double kJoin = 6000;
+struct Choice {
+    int tile;
+    uint32_t splits;
+};
+Choice cheapest_tile(const TileCost (&tiles)[6], int64_t channels, int64_t rows, bool two_digits, int64_t ld, bool may_split) {
+    Choice best = {0, 1};
     double least = 0;
+    const double steps = static_cast<double>(ld) / 64;
     for (int i = 0; i < (two_digits ? 5 : 6); ++i) {   // (two digits are two blocks of 16 rows)
         const double n = static_cast<double>((channels + tiles[i].channels - 1) / tiles[i].channels) * static_cast<double>((rows + tiles[i].tokens - 1) / tiles[i].tokens);
         const double rounds = n <= 256 ? n / 256 : std::ceil(n / 256);   // (256 compute units)
-        const double cost = std::max(tiles[i].alone, rounds * tiles[i].share);
-        if (i == 0 || cost < least) best = i, least = cost;
+        const double cost = std::max(tiles[i].alone, rounds * tiles[i].share) * steps + std::max(1., rounds) * tiles[i].fixed;
+        if (i == 0 || cost < least) best = {i, 1}, least = cost;
+        if (i < 4 || !may_split) continue;
+        const uint32_t splits = static_cast<uint32_t>(std::min({kI8SplitTiles / n, steps / 8, 16.}));
+        if (splits < 2) continue;
+        const double shared = std::max(tiles[i].alone, n * splits / 256 * tiles[i].share) * steps / splits + tiles[i].fixed + kJoin;
+        if (shared < least) best = {i, splits}, least = shared;
     }
     return best;
 }
 
 template <int DIG, bool GATED>
-lordba_status product(const ProductArgs& a, hipStream_t stream) {
-    switch (cheapest_tile(GATED ? kGatedTiles : kTiles, (GATED ? 2 : 1) * a.n, DIG * a.T, DIG == 2)) {
+lordba_status product(ProductArgs a, hipStream_t stream) {
+    const Choice choice = cheapest_tile(GATED ? kGatedTiles : kTiles, (GATED ? 2 : 1) * a.n, DIG * a.T, DIG == 2, a.ld, i8_splits(a.T, a.ld, DIG));
+    a.splits = choice.splits;
+    switch (choice.tile) {
         case 0: return product_launch<256, 256, 4, 2, 1, 4, DIG, GATED>(a, stream);
         case 1: return product_launch<256, 128, 4, 2, 1, 4, DIG, GATED>(a, stream);
         case 2: return product_launch<128, 128, 2, 4, 1, 4, DIG, GATED>(a, stream);
@@ -547,11 +612,18 @@ bool aliased(const Span (&out)[NO], const Span (&in)[NI]) {
 struct Workspace {
     int8_t* q;
     float* scale;
+    uint32_t* arrived;
+    int32_t* parts;
 };
 Workspace split(void* workspace, int64_t T, int64_t cols, int digits) {
     char* const p = static_cast<char*>(workspace);
-    return {reinterpret_cast<int8_t*>(p), reinterpret_cast<float*>(p + i8_scale_offset(T, cols, digits))};
+    char* const more = p + i8_split_offset(T, cols, digits);
+    return {reinterpret_cast<int8_t*>(p), reinterpret_cast<float*>(p + i8_scale_offset(T, cols, digits)), reinterpret_cast<uint32_t*>(more),
+            reinterpret_cast<int32_t*>(more + kI8SplitTiles * 4)};
 }
+
+// The counters that the row kernel clears ahead of the product, where there is room for them.
+uint32_t* split_arrivals(const Workspace& ws, int64_t T, int64_t cols, int digits) { return i8_splits(T, cols, digits) ? ws.arrived : nullptr; }
 
 // y = x diag(col_scale) W^T diag(w_scale) over `contracted` columns
 lordba_status linear(const void* x, const float* col_scale, const int8_t* w, const float* w_scale, void* y, void* workspace, size_t workspace_bytes,
@@ -570,9 +642,9 @@ lordba_status linear(const void* x, const float* col_scale, const int8_t* w, con
     const hipStream_t st = static_cast<hipStream_t>(stream);
     const Workspace ws = split(workspace, T, contracted, digits);
     const ProductArgs a = {w, ws.q, ws.scale, w_scale, nullptr, static_cast<_Float16*>(y), nullptr, T, n, i8_row_bytes(contracted),
-                           static_cast<const _Float16*>(x), contracted};
+                           static_cast<const _Float16*>(x), contracted, ws.parts, ws.arrived, 1, 0};
     if (!col_scale && own_rows_fit<false>(a, digits)) return product_launch<32, 16, 1, 1, 4, 4, 1, false, true>(a, st);
-    const lordba_status rows = lordba_i8_quantize(x, col_scale, ws.q, ws.scale, T, contracted, digits, st);
+    const lordba_status rows = lordba_i8_quantize(x, col_scale, ws.q, ws.scale, split_arrivals(ws, T, contracted, digits), T, contracted, digits, st);
     if (rows != LORDBA_OK) return rows;
     return digits == 1 ? product<1, false>(a, st) : product<2, false>(a, st);
 }
@@ -611,9 +683,9 @@ extern "C" lordba_status lordba_gated_i8(const void* x, const int8_t* W, const f
     const hipStream_t s = static_cast<hipStream_t>(stream);
     const Workspace ws = split(workspace, T, d_in, digits);
     const ProductArgs a = {W, ws.q, ws.scale, w_scale, static_cast<const _Float16*>(addends), static_cast<_Float16*>(h), static_cast<_Float16*>(gate_up),
-                           T, d_ff, i8_row_bytes(d_in), static_cast<const _Float16*>(x), d_in};
+                           T, d_ff, i8_row_bytes(d_in), static_cast<const _Float16*>(x), d_in, ws.parts, ws.arrived, 1, 0};
     if (own_rows_fit<true>(a, digits)) return product_launch<64, 16, 1, 1, 4, 4, 1, true, true>(a, s);
-    if ((st = lordba_i8_quantize(x, nullptr, ws.q, ws.scale, T, d_in, digits, s)) != LORDBA_OK) return st;
+    if ((st = lordba_i8_quantize(x, nullptr, ws.q, ws.scale, split_arrivals(ws, T, d_in, digits), T, d_in, digits, s)) != LORDBA_OK) return st;
     return digits == 1 ? product<1, true>(a, s) : product<2, true>(a, s);
 }
 
@@ -634,7 +706,7 @@ extern "C" lordba_status lordba_gated_i8_backward(const void* dh, const void* ga
     if ((st = check_device()) != LORDBA_OK) return st;
     const hipStream_t s = static_cast<hipStream_t>(stream);
     const Workspace ws = split(workspace, T, 2 * d_ff, digits);
-    if ((st = lordba_i8_gated_grad(dh, gate_up, w_scale, dgate_up, ws.q, ws.scale, T, d_ff, digits, s)) != LORDBA_OK) return st;
-    const ProductArgs a = {Wt, ws.q, ws.scale, nullptr, nullptr, static_cast<_Float16*>(dx), nullptr, T, d_in, i8_row_bytes(2 * d_ff), nullptr, 0};
+    if ((st = lordba_i8_gated_grad(dh, gate_up, w_scale, dgate_up, ws.q, ws.scale, split_arrivals(ws, T, 2 * d_ff, digits), T, d_ff, digits, s)) != LORDBA_OK) return st;
+    const ProductArgs a = {Wt, ws.q, ws.scale, nullptr, nullptr, static_cast<_Float16*>(dx), nullptr, T, d_in, i8_row_bytes(2 * d_ff), nullptr, 0, ws.parts, ws.arrived, 1, 0};
     return digits == 1 ? product<1, false>(a, s) : product<2, false>(a, s);
 }

@@ -1,6 +1,8 @@
 // Row kernels of the 8-bit projections: rows of fp16 numbers into one or two digits, the gradient of the gated activation into two,
 // the layout of weights.  All of them are bound by memory: each reads its input once and holds it in registers while the row's
 // largest magnitude is found.
+#include <algorithm>
+
 #include "lordba_dev_util.h"
 #include "lordba_i8.h"
 
@@ -52,14 +54,22 @@ struct QuantizeArgs {
     const float* col_scale;
     int8_t* q;
     float* scale;
+    uint32_t* clear;
     int64_t rows, cols, ld;
+    int64_t first;   // row of this launch's first workgroup
 };
+
+// kI8SplitTiles counters for the product behind this kernel
+__device__ __forceinline__ void clear_counters(uint32_t* p) {
+    if (p && blockIdx.x == 0 && threadIdx.x < kI8SplitTiles) p[threadIdx.x] = 0;
+}
 
 // NV > 0: a thread's numbers stay in registers between the two passes over the row; NV = 0 (more than 32768 columns): they are read again.
 template <int TPR, int NV, int DIG, bool CS>
 __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void lordba_quantize_rows_kernel(QuantizeArgs a) {
     const int t = threadIdx.x % TPR;
-    const int64_t row = TPR < 256 ? static_cast<int64_t>(blockIdx.x) * (256 / TPR) + threadIdx.x / TPR : blockIdx.x;
+    const int64_t row = a.first + (TPR < 256 ? static_cast<int64_t>(blockIdx.x) * (256 / TPR) + threadIdx.x / TPR : blockIdx.x);
+    clear_counters(a.clear);
     if (row >= a.rows) return;   // (whole waves: a wave has one row)
     const _Float16* x = a.x + row * a.cols;
     const int turns = NV > 0 ? NV : static_cast<int>((a.ld + 8 * TPR - 1) / (8 * TPR));
@@ -103,12 +113,20 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void lordba_quantize_rows_ke
     }
 }
 
+constexpr int64_t kRowsPerLaunch = 1 << 21;   // (a launch counts threads in 32 bits, up to 1024 for a row)
+
 template <int TPR, int NV, int DIG, bool CS>
-lordba_status quantize_launch(const QuantizeArgs& a, hipStream_t stream) {
-    const int64_t per = TPR < 256 ? 256 / TPR : 1;
-    hipLaunchKernelGGL((lordba_quantize_rows_kernel<TPR, NV, DIG, CS>), dim3(static_cast<unsigned>((a.rows + per - 1) / per)),
-                       dim3(TPR < 256 ? 256 : TPR), 0, stream, a);
-    return i8_launched();
+lordba_status quantize_launch(QuantizeArgs a, hipStream_t stream) {
+    constexpr int64_t per = TPR < 256 ? 256 / TPR : 1;
+    for (a.first = 0; a.first < a.rows; a.first += kRowsPerLaunch) {
+        const int64_t n = std::min(kRowsPerLaunch, a.rows - a.first);
+        hipLaunchKernelGGL((lordba_quantize_rows_kernel<TPR, NV, DIG, CS>), dim3(static_cast<unsigned>((n + per - 1) / per)),
+                           dim3(TPR < 256 ? 256 : TPR), 0, stream, a);
+        const lordba_status st = i8_launched();
+        if (st != LORDBA_OK) return st;
+        a.clear = nullptr;
+    }
+    return LORDBA_OK;
 }
 
 template <int DIG, bool CS>
@@ -134,7 +152,9 @@ struct GatedGradArgs {
     _Float16* dgate_up;        // [2, T, d_ff]
     int8_t* q;
     float* scale;
+    uint32_t* clear;
     int64_t T, d_ff, ld;
+    int64_t first;
 };
 
 __device__ __forceinline__ void gated_grad(h8 dh, h8 gate, h8 up, float (&dg)[8], float (&du)[8]) {
@@ -159,11 +179,13 @@ __device__ __forceinline__ void store_bytes(int8_t* p, uint2 v, int64_t n) {
         if (e < n) p[e] = static_cast<int8_t>((e < 4 ? v.x : v.y) >> (8 * (e & 3)));
 }
 
-// NV > 0: a thread's numbers stay in registers; NV = 0 (d_ff > 16384): they are computed again for the second pass
+// Bound by arithmetic (about 30 instructions for a pair of gradients) and memory alike: 2048 rows of 11008 62 us, 315 MB.  NV > 0: a thread's numbers stay in
+// registers (formed again for the second use, 77 us); NV = 0 (d_ff > 16384): they are computed again from memory.
 template <int TPR, int NV, int DIG>
 __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void lordba_gated_grad_kernel(GatedGradArgs a) {
     const int tid = threadIdx.x % TPR;
-    const int64_t row = TPR < 256 ? static_cast<int64_t>(blockIdx.x) * (256 / TPR) + threadIdx.x / TPR : blockIdx.x;
+    const int64_t row = a.first + (TPR < 256 ? static_cast<int64_t>(blockIdx.x) * (256 / TPR) + threadIdx.x / TPR : blockIdx.x);
+    clear_counters(a.clear);
     if (row >= a.T) return;   // (whole waves: a wave has one row)
     const int64_t F = a.d_ff, plane = a.T * F;
     const _Float16 *dh = a.dh + row * F, *gate = a.gate_up + row * F, *up = gate + plane;
@@ -230,19 +252,33 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void lordba_gated_grad_kerne
     }
 }
 
+template <int TPR, int NV, int DIG>
+lordba_status gated_grad_launch(GatedGradArgs a, hipStream_t stream) {
+    constexpr int64_t per = TPR < 256 ? 256 / TPR : 1;
+    for (a.first = 0; a.first < a.T; a.first += kRowsPerLaunch) {
+        const int64_t n = std::min(kRowsPerLaunch, a.T - a.first);
+        hipLaunchKernelGGL((lordba_gated_grad_kernel<TPR, NV, DIG>), dim3(static_cast<unsigned>((n + per - 1) / per)), dim3(TPR < 256 ? 256 : TPR), 0,
+                           stream, a);
+        const lordba_status st = i8_launched();
+        if (st != LORDBA_OK) return st;
+        a.clear = nullptr;
+    }
+    return LORDBA_OK;
+}
+
+// With many rows of up to 1024 columns a wave has a row of its own (16384 x 320: 58 -> 27 us for the call); few rows are done sooner by more waves (190 x 811
+// 8.7 -> 5.8 us).  (1024 threads of two groups each, for the longest rows, spilled:
+// 72 us instead of 62 at 2048 x 11008.)
 template <int DIG>
-lordba_status gated_grad_launch(const GatedGradArgs& a, hipStream_t stream) {
-    const dim3 grid(static_cast<unsigned>(a.T)), waves(static_cast<unsigned>((a.T + 3) / 4));
-    // Up to 1024 columns a wave has a row of its own (16384 x 320: 58 -> 27 us for the call).  (1024 threads of two groups each, for the longest rows, spilled: 72 us instead
-    // of 62 at 2048 x 11008.)
-    if (a.d_ff <= 512) hipLaunchKernelGGL((lordba_gated_grad_kernel<64, 1, DIG>), waves, dim3(256), 0, stream, a);
-    else if (a.d_ff <= 1024) hipLaunchKernelGGL((lordba_gated_grad_kernel<64, 2, DIG>), waves, dim3(256), 0, stream, a);
-    else if (a.d_ff <= 2048) hipLaunchKernelGGL((lordba_gated_grad_kernel<256, 1, DIG>), grid, dim3(256), 0, stream, a);
-    else if (a.d_ff <= 4096) hipLaunchKernelGGL((lordba_gated_grad_kernel<512, 1, DIG>), grid, dim3(512), 0, stream, a);
-    else if (a.d_ff <= 8192) hipLaunchKernelGGL((lordba_gated_grad_kernel<512, 2, DIG>), grid, dim3(512), 0, stream, a);
-    else if (a.d_ff <= 16384) hipLaunchKernelGGL((lordba_gated_grad_kernel<512, 4, DIG>), grid, dim3(512), 0, stream, a);
-    else hipLaunchKernelGGL((lordba_gated_grad_kernel<512, 0, DIG>), grid, dim3(512), 0, stream, a);
-    return i8_launched();
+lordba_status gated_grad(const GatedGradArgs& a, hipStream_t stream) {
+    const bool many = a.T >= 512;
+    if (many && a.d_ff <= 512) return gated_grad_launch<64, 1, DIG>(a, stream);
+    if (many && a.d_ff <= 1024) return gated_grad_launch<64, 2, DIG>(a, stream);
+    if (a.d_ff <= 2048) return gated_grad_launch<256, 1, DIG>(a, stream);
+    if (a.d_ff <= 4096) return gated_grad_launch<512, 1, DIG>(a, stream);
+    if (a.d_ff <= 8192) return gated_grad_launch<512, 2, DIG>(a, stream);
+    if (a.d_ff <= 16384) return gated_grad_launch<512, 4, DIG>(a, stream);
+    return gated_grad_launch<512, 0, DIG>(a, stream);
 }
 
 // ---- layout of weights --------------------------------------------------------------------------------------------
@@ -282,18 +318,18 @@ __global__ __launch_bounds__(256) void lordba_transpose_i8_kernel(LayoutArgs a) 
 
 }  // namespace
 
-lordba_status lordba_i8_quantize(const void* x, const float* col_scale, int8_t* q, float* scale, int64_t rows, int64_t cols, int digits,
-                                 hipStream_t stream) {
-    const QuantizeArgs a = {static_cast<const _Float16*>(x), col_scale, q, scale, rows, cols, i8_row_bytes(cols)};
+lordba_status lordba_i8_quantize(const void* x, const float* col_scale, int8_t* q, float* scale, uint32_t* clear, int64_t rows, int64_t cols,
+                                 int digits, hipStream_t stream) {
+    const QuantizeArgs a = {static_cast<const _Float16*>(x), col_scale, q, scale, clear, rows, cols, i8_row_bytes(cols), 0};
     if (digits == 1) return col_scale ? quantize<1, true>(a, stream) : quantize<1, false>(a, stream);
     return col_scale ? quantize<2, true>(a, stream) : quantize<2, false>(a, stream);
 }
 
 lordba_status lordba_i8_gated_grad(const void* dh, const void* gate_up, const float* w_scale, void* dgate_up, int8_t* q, float* scale,
-                                   int64_t T, int64_t d_ff, int digits, hipStream_t stream) {
+                                   uint32_t* clear, int64_t T, int64_t d_ff, int digits, hipStream_t stream) {
     const GatedGradArgs a = {static_cast<const _Float16*>(dh), static_cast<const _Float16*>(gate_up), w_scale, static_cast<_Float16*>(dgate_up),
-                             q, scale, T, d_ff, i8_row_bytes(2 * d_ff)};
-    return digits == 1 ? gated_grad_launch<1>(a, stream) : gated_grad_launch<2>(a, stream);
+                             q, scale, clear, T, d_ff, i8_row_bytes(2 * d_ff), 0};
+    return digits == 1 ? gated_grad<1>(a, stream) : gated_grad<2>(a, stream);
 }
 
 extern "C" size_t lordba_i8_row_bytes(int64_t cols) {
@@ -302,7 +338,7 @@ extern "C" size_t lordba_i8_row_bytes(int64_t cols) {
 
 extern "C" size_t lordba_i8_workspace_bytes(int64_t T, int64_t cols, int digits) {
     if (T < 0 || T > INT32_MAX || cols < 1 || cols > LORDBA_I8_MAX_COLUMNS || digits < 1 || digits > 2) return 0;
-    return i8_scale_offset(T, cols, digits) + static_cast<size_t>(T) * 4;
+    return i8_workspace_bytes(T, cols, digits);
 }
 
 extern "C" lordba_status lordba_quantize_rows(const void* x, const float* col_scale, int8_t* q, float* scale, int64_t rows, int64_t cols,
@@ -318,7 +354,7 @@ extern "C" lordba_status lordba_quantize_rows(const void* x, const float* col_sc
         return LORDBA_ERR_ALIAS;
     const lordba_status dev = check_device();
     if (dev != LORDBA_OK) return dev;
-    return lordba_i8_quantize(x, col_scale, q, scale, rows, cols, digits, static_cast<hipStream_t>(stream));
+    return lordba_i8_quantize(x, col_scale, q, scale, nullptr, rows, cols, digits, static_cast<hipStream_t>(stream));
 }
 
 extern "C" lordba_status lordba_layout_i8(const int8_t* w, int8_t* out, int64_t rows, int64_t cols, int transposed, void* stream) {

@@ -174,6 +174,56 @@ def test_linear_backward(torch, shape, digits):
         assert np.array_equal(dx, host(binding.lordba_linear_i8_backward(g, Wt, sd)))   # (the default)
 
 
+# Every tile and way of working: 256 x 256 (whole, ragged, odd widths), 256 x 128, 128 x 128, 64 x 64 and below, steps shared by several workgroups (few rows
+# or columns, long contractions), and a few tokens whose rows the product's workgroups make (multiples of 8 columns, 16-byte aligned)
+REGIMES = [(2100, 300, 4200), (2048, 520, 4095), (1030, 260, 4100), (512, 700, 4096), (600, 250, 1111), (40, 5000, 70), (3, 9000, 40), (16, 131071, 3), (20, 3000, 33),
+           (130, 2100, 20), (1, 4096, 515), (2, 6000, 100), (7, 1024, 64), (1, 13824, 33), (3, 4104, 37), (16, 64, 8), (16, 880, 31)]
+
+
+@pytest.mark.parametrize("digits", [1, 2])
+@pytest.mark.parametrize("shape", REGIMES, ids=lambda s: "T%d_%dx%d" % s)
+def test_linear_regimes(torch, shape, digits):
+    T, d_in, d_out = shape
+    rng = np.random.default_rng(T + 23 * d_in + 29 * d_out)
+    W, ws = weights(rng, d_out, d_in)
+    Wl = binding.lordba_layout_i8(torch.from_numpy(W).cuda())
+    x, sd = torch.from_numpy(acts(rng, T, d_in)).cuda(), torch.from_numpy(ws).cuda()
+    y = binding.lordba_linear_i8(x, Wl, sd, digits=digits)
+    near(host(y), *product(*integers(torch, x, None, digits), W, ws))
+    for _ in range(2):   # the same again, in a workspace that holds anything
+        junk = torch.full((binding.lordba_i8_workspace_bytes(T, d_in, digits),), 0xA5, dtype=torch.uint8, device="cuda")
+        assert torch.equal(binding.lordba_linear_i8(x, Wl, sd, digits=digits, workspace=junk), y)
+
+
+@pytest.mark.parametrize("shape", [(2053, 320, 4096), (2048, 256, 4090), (1024, 300, 3001), (512, 260, 2048), (4, 6000, 30), (20, 3000, 17), (1, 4096, 100), (3, 2048, 50),
+                                   (1, 6144, 9)], ids=lambda s: "T%d_%dx%d" % s)
+def test_gated_regimes(torch, shape):
+    T, d_in, F = shape
+    rng = np.random.default_rng(T + 31 * d_in + 37 * F)
+    W, ws = weights(rng, 2 * F, d_in)
+    Wl, sd = binding.lordba_layout_i8(torch.from_numpy(W).cuda()), torch.from_numpy(ws).cuda()
+    x, add = torch.from_numpy(acts(rng, T, d_in)).cuda(), acts(rng, 2 * T, F, zero_rows=False).reshape(2, T, F)
+    ad = torch.from_numpy(add).cuda()
+    h, kept = binding.lordba_gated_i8(x, Wl, sd, addends=ad, save=True)
+    gate, up, want, eg, eu = gated(*integers(torch, x, None, 1), W, ws, add, F)
+    near(host(kept)[0], gate, eg)
+    near(host(kept)[1], up, eu)
+    silu = np.abs(gate) / (1 + np.exp(-gate))
+    near(host(h), want, 1.1 * np.abs(up) * eg + silu * eu + np.abs(want) * 2.0 ** -18 * (1 + np.abs(gate) / 16))
+    # addends that start in the middle of a word take another way to the same sums
+    other = place(torch, add, 1)
+    h2, kept2 = binding.lordba_gated_i8(x, Wl, sd, addends=other, save=True)
+    assert torch.equal(h2, h) and torch.equal(kept2, kept)
+    none = binding.lordba_gated_i8(x, Wl, sd)
+    zero = binding.lordba_gated_i8(x, Wl, sd, addends=torch.zeros_like(ad))
+    assert torch.equal(none, zero)
+
+
+@pytest.mark.parametrize("shape", [(4, 83, 12871), (3, 65, 6926), (70, 30, 3000), (1100, 2100, 130)], ids=lambda s: "T%d_%dx%d" % s)
+def test_gated_backward_regimes(torch, shape):
+    test_gated_backward(torch, shape, 2)
+
+
 def test_the_linear_gradient_is_the_difference(torch):
     # y is linear in x: <dx, v> = <g, W v> for any v, here v of the size of x
     rng = np.random.default_rng(3)
