@@ -579,11 +579,11 @@ lordba_status product(ProductArgs a, hipStream_t stream) {
 
 // Whether the product's workgroups bring the rows to digits themselves: one launch instead of two, but every workgroup does the whole of it.  Times of a
 // call in us, with the row kernel -> without, T x d_in -> d_out: 1 x 4096 -> 4096 7.9 -> 5.8, 1 x 4096 -> 11008 12.2 -> 8.9, 1 x 11008 -> 4096 13.2 -> 11.7,
-// 2 x 4096 -> 4096 8.0 -> 6.8, 2 x 11008 -> 4096 13.1 -> 13.6, 4 x 1000 -> 1024 8.2 -> 5.9, 4 x 4096 -> 11008 12.4 -> 17.8; gated, 1 x 4096 x 11008
-// 19.6 -> 17.2, 2 x 4096 x 11008 19.4 -> 21.9.
+// 2 x 4096 -> 4096 8.0 -> 6.8, 2 x 11008 -> 4096 13.1 -> 13.6, 4 x 1000 -> 1024 8.2 -> 5.9, 4 x 4096 -> 11008 12.4 -> 17.8, 16 x 512 -> 512 8.5 -> 12.9 (tokens are
+// taken one after the other); gated, 1 x 4096 x 11008 19.6 -> 17.2, 2 x 4096 x 11008 19.4 -> 21.9.
 template <bool GATED>
 bool own_rows_fit(const ProductArgs& a, int digits) {
-    return digits == 1 && a.T <= 16 && a.T * a.d_in <= (GATED ? 6144 : 14336) && a.d_in % 8 == 0 && !i8_misaligned(a.x, 16) &&
+    return digits == 1 && a.T <= 4 && a.T * a.d_in <= (GATED ? 6144 : 14336) && a.d_in % 8 == 0 && !i8_misaligned(a.x, 16) &&
            static_cast<size_t>(own_bytes(a.T, a.d_in, a.ld)) + 4 * 4 * (GATED ? 64 : 32) * 64 <= kLdsBytes;
 }
 
