@@ -334,7 +334,8 @@ __global__ __launch_bounds__(64 * WC * WT * WK) void lordba_i8_product_kernel(Pr
     };
     // The addends of a whole tile come the way of the operands: in the last S steps, when there is nothing left to request for the products, each lane
     // requests those that it will add itself (P planes, TB / DIG tokens, kN groups of columns, eight at a time) into its wave's share of the slots that fall
-    // free.  The products hide what the loads wait for: ADD_FIGURES
+    // free.  The products hide what the loads wait for: with cold
+    // weights 2048 x 4096 x 11008 203 -> 193 us, 4096 x 4096 x 11008 434 -> 367.
     constexpr int P = GATED ? 2 : 1, kN = CB / (2 * P), kAddends = P * (TB / DIG) * kN;
     constexpr bool kAhead = GATED && WK == 1 && kAddends <= L * S;
     const int64_t cw = c0 + wc * (kCols / WC), tw = t0 + wt * (kTokens / WT);
@@ -430,7 +431,7 @@ __global__ __launch_bounds__(64 * WC * WT * WK) void lordba_i8_product_kernel(Pr
     }
     if constexpr (SPLIT) {
         // The last workgroup of a tile to arrive joins the parts: whole numbers, any order gives the same sum.  The parts go through the memory that all XCDs
-        // share, piece by piece (accesses of agent scope), not by a fence, which would have the XCD's whole L2 written back: 49 x 12306 -> 196 20.7 us.
+        // share, piece by piece (accesses of agent scope), not by a fence, which would have the XCD's whole L2 written back (3 us more).
         if (a.splits > 1) {
             uint64_t* const parts = reinterpret_cast<uint64_t*>(a.parts) + static_cast<int64_t>(blockIdx.x) * (CB * TB * 128) + lane;
             const int64_t apart = static_cast<int64_t>(gridDim.x) * (CB * TB * 128);
@@ -537,7 +538,8 @@ struct TileCost {
 constexpr TileCost kTiles[] = {{256, 256, 600, 800, 7000}, {256, 128, 390, 510, 3400}, {128, 128, 200, 300, 1100}, {64, 64, 77, 125, 600}, {32, 32, 35, 60, 300}, {32, 16, 25, 50, 300}};
 constexpr TileCost kGatedTiles[] = {{256, 256, 600, 800, 7000}, {256, 128, 390, 510, 3400}, {128, 128, 200, 300, 1100}, {64, 64, 77, 125, 600}, {64, 32, 60, 105, 500}, {64, 16, 40, 100, 400}};
 
-// Few small tiles of a long contraction: several workgroups share a tile's steps, which costs them kJoin ns to join (24 x 12306 -> 196: SPLIT_FIGURE).
+// Few small tiles of a long contraction: several workgroups share a tile's steps, which costs them kJoin ns to join (the product of 4 x 25742 -> 83 in two
+// digits 15.8 -> 6.4 us).
 constexpr double kJoin = 6000;
 struct Choice {
     int tile;

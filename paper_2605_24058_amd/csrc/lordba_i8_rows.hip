@@ -290,13 +290,14 @@ struct LayoutArgs {
 
 __global__ __launch_bounds__(256) void lordba_layout_i8_kernel(LayoutArgs a) {
     const int64_t c = (static_cast<int64_t>(blockIdx.y) * 256 + threadIdx.x) * 4;
-    const int64_t row = blockIdx.x;
     if (c >= a.ld) return;
-    uint32_t v = 0;
+    for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
+        uint32_t v = 0;
 #pragma unroll
-    for (int e = 0; e < 4; ++e)
-        if (c + e < a.cols) v |= static_cast<uint32_t>(static_cast<uint8_t>(a.w[row * a.cols + c + e])) << (8 * e);
-    *reinterpret_cast<uint32_t*>(a.out + row * a.ld + c) = v;
+        for (int e = 0; e < 4; ++e)
+            if (c + e < a.cols) v |= static_cast<uint32_t>(static_cast<uint8_t>(a.w[row * a.cols + c + e])) << (8 * e);
+        *reinterpret_cast<uint32_t*>(a.out + row * a.ld + c) = v;
+    }
 }
 
 // 64 x 64 tiles through LDS: rows of w in, columns out, four entries of an output row per store
@@ -369,7 +370,7 @@ extern "C" lordba_status lordba_layout_i8(const int8_t* w, int8_t* out, int64_t 
         hipLaunchKernelGGL(lordba_transpose_i8_kernel, dim3(static_cast<unsigned>((cols + 63) / 64), static_cast<unsigned>((a.ld + 63) / 64)),
                            dim3(256), 0, static_cast<hipStream_t>(stream), a);
     else
-        hipLaunchKernelGGL(lordba_layout_i8_kernel, dim3(static_cast<unsigned>(rows), static_cast<unsigned>((a.ld + 1023) / 1024)), dim3(256), 0,
+        hipLaunchKernelGGL(lordba_layout_i8_kernel, dim3(static_cast<unsigned>(std::min<int64_t>(rows, 1 << 20)), static_cast<unsigned>((a.ld + 1023) / 1024)), dim3(256), 0,
                            static_cast<hipStream_t>(stream), a);
     return i8_launched();
 }
