@@ -529,14 +529,16 @@ lordba_status product_launch(const ProductArgs& a, hipStream_t stream) {
     return LORDBA_OK;
 }
 
-// The tiles and their times on a compute unit, in nanoseconds: a step of 64 columns alone on a chip with few workgroups (waiting), the same as a share of
-// a chip that is full (throughput; small tiles run side by side on a unit), and the filling and emptying around the steps.
+// The tiles and their times on a compute unit, in nanoseconds: a step of 64 columns alone on a chip with few workgroups (waiting; 1.4 times that where the
+// weights are read once, from memory), the same as a share of a chip that is full (throughput; small tiles run side by side on a unit), and what comes around
+// the steps, filling and results.  Fitted to some forty shapes of 1 to 16384 rows, 64 to 13824 columns, even and odd; the tile with the least sum was the
+// fastest of the six or within 15 % of it on all but a few of them (6536 x 129 x 1910 gated: 26 us instead of 19).
 struct TileCost {
     int channels, tokens;
     double alone, share, fixed;
 };
 constexpr TileCost kTiles[] = {{256, 256, 600, 800, 7000}, {256, 128, 390, 510, 3400}, {128, 128, 200, 300, 1100}, {64, 64, 77, 125, 600}, {32, 32, 35, 60, 300}, {32, 16, 25, 50, 300}};
-constexpr TileCost kGatedTiles[] = {{256, 256, 600, 800, 7000}, {256, 128, 390, 510, 3400}, {128, 128, 200, 300, 1100}, {64, 64, 77, 125, 600}, {64, 32, 60, 105, 500}, {64, 16, 40, 100, 400}};
+constexpr TileCost kGatedTiles[] = {{256, 256, 600, 800, 18000}, {256, 128, 390, 510, 9500}, {128, 128, 200, 300, 5000}, {64, 64, 77, 125, 1500}, {64, 32, 60, 105, 1000}, {64, 16, 40, 100, 600}};
 
 // Few small tiles of a long contraction: several workgroups share a tile's steps, which costs them kJoin ns to join (the product of 4 x 25742 -> 83 in two
 // digits 15.8 -> 6.4 us).
@@ -550,14 +552,16 @@ Choice cheapest_tile(const TileCost (&tiles)[6], int64_t channels, int64_t rows,
     double least = 0;
     const double steps = static_cast<double>(ld) / 64;
     for (int i = 0; i < (two_digits ? 5 : 6); ++i) {   // (two digits are two blocks of 16 rows)
-        const double n = static_cast<double>((channels + tiles[i].channels - 1) / tiles[i].channels) * static_cast<double>((rows + tiles[i].tokens - 1) / tiles[i].tokens);
+        const int64_t across = (rows + tiles[i].tokens - 1) / tiles[i].tokens;
+        const double n = static_cast<double>((channels + tiles[i].channels - 1) / tiles[i].channels) * static_cast<double>(across);
+        const double alone = across == 1 ? 1.4 * tiles[i].alone : tiles[i].alone;
         const double rounds = n <= 256 ? n / 256 : std::ceil(n / 256);   // (256 compute units)
-        const double cost = std::max(tiles[i].alone, rounds * tiles[i].share) * steps + std::max(1., rounds) * tiles[i].fixed;
+        const double cost = std::max(alone, rounds * tiles[i].share) * steps + std::max(1., rounds) * tiles[i].fixed;
         if (i == 0 || cost < least) best = {i, 1}, least = cost;
         if (i < 4 || !may_split) continue;
         const uint32_t splits = static_cast<uint32_t>(std::min({kI8SplitTiles / n, steps / 8, 16.}));
         if (splits < 2) continue;
-        const double shared = std::max(tiles[i].alone, n * splits / 256 * tiles[i].share) * steps / splits + tiles[i].fixed + kJoin;
+        const double shared = std::max(alone, n * splits / 256 * tiles[i].share) * steps / splits + tiles[i].fixed + kJoin;
         if (shared < least) best = {i, splits}, least = shared;
     }
     return best;
