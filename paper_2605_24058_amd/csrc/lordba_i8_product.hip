@@ -24,6 +24,7 @@ struct ProductArgs {
     _Float16* y;              // [T, n]
     _Float16* kept;           // gated: [2, T, n], or null
     int64_t T, n, ld;
+    int pieces;               // of 64 columns that the contraction has (behind them the rows are zeros)
     const _Float16* x;        // OWN_ROWS: [T, d_in], in place of q and q_scale
     int64_t d_in;
     int32_t* parts;           // splits > 1: [splits, tiles, 16 x 16 blocks] sums, behind the tiles' counters of arrivals (zeros)
@@ -269,7 +270,7 @@ __global__ __launch_bounds__(64 * WC * WT * WK) void lordba_i8_product_kernel(Pr
     const int64_t c0 = static_cast<int64_t>(tile.c) * kCols, t0 = static_cast<int64_t>(tile.t) * kTokens;
     // (SPLIT: this workgroup has the steps k0 .. k0 + K - 1 of the contraction)
     constexpr bool SPLIT = WC * WT == 1 && WK > 1 && !OWN_ROWS;
-    const int steps = static_cast<int>(a.ld / (64 * WK));
+    const int steps = (a.pieces + WK - 1) / WK;
     const int k0 = SPLIT ? static_cast<int>(static_cast<int64_t>(steps) * blockIdx.y / a.splits) : 0;
     const int K = SPLIT ? static_cast<int>(static_cast<int64_t>(steps) * (blockIdx.y + 1) / a.splits) - k0 : steps;
 
@@ -547,10 +548,10 @@ struct Choice {
     int tile;
     uint32_t splits;
 };
-Choice cheapest_tile(const TileCost (&tiles)[6], int64_t channels, int64_t rows, bool two_digits, int64_t ld, bool may_split) {
+Choice cheapest_tile(const TileCost (&tiles)[6], int64_t channels, int64_t rows, bool two_digits, int pieces, bool may_split) {
     Choice best = {0, 1};
     double least = 0;
-    const double steps = static_cast<double>(ld) / 64;
+    const double steps = pieces;
     for (int i = 0; i < (two_digits ? 5 : 6); ++i) {   // (two digits are two blocks of 16 rows)
         const int64_t across = (rows + tiles[i].tokens - 1) / tiles[i].tokens;
         const double n = static_cast<double>((channels + tiles[i].channels - 1) / tiles[i].channels) * static_cast<double>(across);
@@ -569,7 +570,7 @@ Choice cheapest_tile(const TileCost (&tiles)[6], int64_t channels, int64_t rows,
 
 template <int DIG, bool GATED>
 lordba_status product(ProductArgs a, hipStream_t stream) {
-    const Choice choice = cheapest_tile(GATED ? kGatedTiles : kTiles, (GATED ? 2 : 1) * a.n, DIG * a.T, DIG == 2, a.ld, i8_splits(a.T, a.ld, DIG));
+    const Choice choice = cheapest_tile(GATED ? kGatedTiles : kTiles, (GATED ? 2 : 1) * a.n, DIG * a.T, DIG == 2, a.pieces, i8_splits(a.T, a.ld, DIG));
     a.splits = choice.splits;
     switch (choice.tile) {
         case 0: return product_launch<256, 256, 4, 2, 1, 4, DIG, GATED>(a, stream);
@@ -647,7 +648,7 @@ lordba_status linear(const void* x, const float* col_scale, const int8_t* w, con
     if (dev != LORDBA_OK) return dev;
     const hipStream_t st = static_cast<hipStream_t>(stream);
     const Workspace ws = split(workspace, T, contracted, digits);
-    const ProductArgs a = {w, ws.q, ws.scale, w_scale, nullptr, static_cast<_Float16*>(y), nullptr, T, n, i8_row_bytes(contracted),
+    const ProductArgs a = {w, ws.q, ws.scale, w_scale, nullptr, static_cast<_Float16*>(y), nullptr, T, n, i8_row_bytes(contracted), static_cast<int>((contracted + 63) / 64),
                            static_cast<const _Float16*>(x), contracted, ws.parts, ws.arrived, 1, 0};
     if (!col_scale && own_rows_fit<false>(a, digits)) return product_launch<32, 16, 1, 1, 4, 4, 1, false, true>(a, st);
     const lordba_status rows = lordba_i8_quantize(x, col_scale, ws.q, ws.scale, split_arrivals(ws, T, contracted, digits), T, contracted, digits, st);
@@ -689,7 +690,7 @@ extern "C" lordba_status lordba_gated_i8(const void* x, const int8_t* W, const f
     const hipStream_t s = static_cast<hipStream_t>(stream);
     const Workspace ws = split(workspace, T, d_in, digits);
     const ProductArgs a = {W, ws.q, ws.scale, w_scale, static_cast<const _Float16*>(addends), static_cast<_Float16*>(h), static_cast<_Float16*>(gate_up),
-                           T, d_ff, i8_row_bytes(d_in), static_cast<const _Float16*>(x), d_in, ws.parts, ws.arrived, 1, 0};
+                           T, d_ff, i8_row_bytes(d_in), static_cast<int>((d_in + 63) / 64), static_cast<const _Float16*>(x), d_in, ws.parts, ws.arrived, 1, 0};
     if (own_rows_fit<true>(a, digits)) return product_launch<64, 16, 1, 1, 4, 4, 1, true, true>(a, s);
     if ((st = lordba_i8_quantize(x, nullptr, ws.q, ws.scale, split_arrivals(ws, T, d_in, digits), T, d_in, digits, s)) != LORDBA_OK) return st;
     return digits == 1 ? product<1, true>(a, s) : product<2, true>(a, s);
@@ -713,6 +714,6 @@ extern "C" lordba_status lordba_gated_i8_backward(const void* dh, const void* ga
     const hipStream_t s = static_cast<hipStream_t>(stream);
     const Workspace ws = split(workspace, T, 2 * d_ff, digits);
     if ((st = lordba_i8_gated_grad(dh, gate_up, w_scale, dgate_up, ws.q, ws.scale, split_arrivals(ws, T, 2 * d_ff, digits), T, d_ff, digits, s)) != LORDBA_OK) return st;
-    const ProductArgs a = {Wt, ws.q, ws.scale, nullptr, nullptr, static_cast<_Float16*>(dx), nullptr, T, d_in, i8_row_bytes(2 * d_ff), nullptr, 0, ws.parts, ws.arrived, 1, 0};
+    const ProductArgs a = {Wt, ws.q, ws.scale, nullptr, nullptr, static_cast<_Float16*>(dx), nullptr, T, d_in, i8_row_bytes(2 * d_ff), static_cast<int>((2 * d_ff + 63) / 64), nullptr, 0, ws.parts, ws.arrived, 1, 0};
     return digits == 1 ? product<1, false>(a, s) : product<2, false>(a, s);
 }
