@@ -13,7 +13,7 @@
  *     B1 in {+-1}^{N x R}   ->  S_A = B1^T, logical shape [r, d_in]
  *     B2 in {+-1}^{R x M}   ->  S_B = B2^T, logical shape [d_out, r]
  *     alpha, beta, gamma    ->  s_in[d_in], s_rank[r], s_out[d_out]   (fp16, any finite real value)
- *     W0^T x (base output)  ->  y_base (an input; the base GEMM is not part of this library)
+ *     W0^T x (base output)  ->  y_base (an input; on 8-bit weights lordba_linear_i8 computes it)
  *
  * Canonical packed carrier format (the paper says only "bit-packed", Sec. 3.3; storage is
  * R(N+M) bits, Eq. (lordba-bits)).  A [rows, cols] sign matrix is the row-major bit stream

@@ -5,6 +5,7 @@
 // 256 hi + lo of neighbouring accumulators), in the gated block the weight blocks alternate gate, up, so that a lane holds both
 // factors of its outputs.
 #include <algorithm>
+#include <atomic>
 #include <cmath>
 #include <type_traits>
 
@@ -509,11 +510,17 @@ lordba_status product_launch(const ProductArgs& a, hipStream_t stream) {
     constexpr size_t kRing = S * WK * (OWN_ROWS ? CT : CT + TT) * 64;
     const size_t lds = kRing + (OWN_ROWS ? static_cast<size_t>(own_bytes(a.T, a.d_in, a.ld)) : 0);
     static_assert(kRing <= kLdsBytes, "LDS of a compute unit");
-    if (OWN_ROWS || kRing > 64 * 1024) {
-        if (hipFuncSetAttribute(reinterpret_cast<const void*>(lordba_i8_product_kernel<CT, TT, WC, WT, WK, S, DIG, GATED, OWN_ROWS>),
-                                hipFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(OWN_ROWS ? kLdsBytes : kRing)) != hipSuccess) {
-            (void)hipGetLastError();
-            return LORDBA_ERR_LAUNCH;
+    if (OWN_ROWS || kRing > 64 * 1024) {   // (once for a device: more LDS than a launch gets unasked)
+        static std::atomic<uint64_t> asked{0};
+        int device = 0;
+        if (hipGetDevice(&device) != hipSuccess || device < 0 || device >= 64) return LORDBA_ERR_NO_DEVICE;
+        if (!(asked.load(std::memory_order_relaxed) >> device & 1)) {
+            if (hipFuncSetAttribute(reinterpret_cast<const void*>(lordba_i8_product_kernel<CT, TT, WC, WT, WK, S, DIG, GATED, OWN_ROWS>),
+                                    hipFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(OWN_ROWS ? kLdsBytes : kRing)) != hipSuccess) {
+                (void)hipGetLastError();
+                return LORDBA_ERR_LAUNCH;
+            }
+            asked.fetch_or(static_cast<uint64_t>(1) << device, std::memory_order_relaxed);
         }
     }
     const int64_t tiles = (a.n + kCols - 1) / kCols * ((a.T + kTokens - 1) / kTokens);

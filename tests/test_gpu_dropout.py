@@ -116,15 +116,16 @@ def test_the_backward_pass_is_the_forward_pass_on_the_gradient(torch):
 
 
 @pytest.mark.gpu
-def test_more_than_32_bits_of_elements(torch):
-    n, p, seed = (1 << 32) + 4104, 0.25, 77
+@pytest.mark.parametrize("n", [(1 << 32) + 4104, (1 << 34) + 4104], ids=["2^32", "2^34"])   # (the second takes two launches)
+def test_more_than_32_bits_of_elements(torch, n):
+    p, seed = 0.25, 77
     x = torch.ones(n, dtype=torch.float16, device="cuda")
     y = binding.lordba_dropout(x, p, seed, 3, y_out=x)
-    for start in (0, (1 << 31) - 64, (1 << 32) - 64, (1 << 32) + 4000):
+    for start in (0, (1 << 31) - 64, (1 << 32) - 64, (1 << 32) + 4000, (n - 4104) - 64, n - 104):
         m = min(128, n - start)
         got = y[start:start + m].cpu().numpy()
         assert np.array_equal(got != 0, draws(start, m, seed, 3) >= 16384)
-    share = float((y != 0).sum()) / n
+    share = sum(float((part != 0).sum()) for part in y.split(1 << 31)) / n
     assert abs(share - 0.75) <= 6 * np.sqrt(0.75 * 0.25 / n)
     assert binding.lordba_dropout(x[:0], p, seed).numel() == 0
 

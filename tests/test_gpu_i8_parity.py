@@ -399,6 +399,22 @@ def test_matrices_past_4_gib(torch):
     near(host(y[pick]), *product(*integers(torch, some, None, 1), host(w), np.full(5, 1e-3, np.float32)))
 
 
+def test_more_rows_than_a_launch(torch):
+    # the row kernels take 2^21 rows a launch
+    T, d_in, F = (1 << 21) + 77, 3, 4
+    rng = np.random.default_rng(9)
+    W, ws = weights(rng, 2 * F, d_in)
+    Wt, sd = binding.lordba_layout_i8(torch.from_numpy(W).cuda(), True), torch.from_numpy(ws).cuda()
+    gen = torch.Generator(device="cuda").manual_seed(2)
+    dh, gu = torch.randn(T, F, generator=gen, device="cuda").half(), torch.randn(2, T, F, generator=gen, device="cuda").half()
+    dx, dgu = binding.lordba_gated_i8_backward(dh, gu, Wt, sd)
+    pick = torch.tensor([0, 1, (1 << 21) - 1, 1 << 21, (1 << 21) + 1, T - 1], device="cuda")
+    one, many = binding.lordba_gated_i8_backward(dh[pick], gu[:, pick].contiguous(), Wt, sd)
+    assert torch.equal(dx[pick], one) and torch.equal(dgu[:, pick], many)
+    d, gate, up = host(dh[pick]).astype(np.float64), *host(gu[:, pick]).astype(np.float64)
+    near(host(many)[0], gated_loss_parts(d, gate, up)[0], np.abs(d * up) * 2.0 ** -17 * (1 + np.abs(gate)))
+
+
 def test_streams_and_graphs(torch):
     rng = np.random.default_rng(6)
     T, d_in, F = 50, 300, 90
