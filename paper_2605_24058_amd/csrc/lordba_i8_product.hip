@@ -545,8 +545,10 @@ struct TileCost {
     int channels, tokens;
     double alone, share, fixed;
 };
-constexpr TileCost kTiles[] = {{256, 256, 600, 800, 7000}, {256, 128, 390, 510, 3400}, {128, 128, 200, 300, 1100}, {64, 64, 77, 125, 600}, {32, 32, 35, 60, 300}, {32, 16, 25, 50, 300}};
-constexpr TileCost kGatedTiles[] = {{256, 256, 600, 800, 18000}, {256, 128, 390, 510, 9500}, {128, 128, 200, 300, 5000}, {64, 64, 77, 125, 1500}, {64, 32, 60, 105, 1000}, {64, 16, 40, 100, 600}};
+constexpr TileCost kTiles[7] = {{256, 256, 600, 800, 7000}, {256, 128, 390, 510, 3400}, {128, 128, 200, 300, 1100}, {64, 64, 77, 125, 600},
+                                {32, 64, 55, 80, 400},      {32, 32, 35, 60, 300},      {32, 16, 25, 50, 300}};
+constexpr TileCost kGatedTiles[7] = {{256, 256, 600, 800, 18000}, {256, 128, 390, 510, 9500}, {128, 128, 200, 300, 5000}, {64, 64, 77, 125, 1500},
+                                     {64, 32, 60, 105, 1000},     {64, 32, 60, 105, 1000},    {64, 16, 40, 100, 600}};   // (64 x 32 stands for both small plain ones)
 
 // Few small tiles of a long contraction: several workgroups share a tile's steps, which costs them kJoin ns to join (the product of 4 x 25742 -> 83 in two
 // digits 15.8 -> 6.4 us).
@@ -555,18 +557,18 @@ struct Choice {
     int tile;
     uint32_t splits;
 };
-Choice cheapest_tile(const TileCost (&tiles)[6], int64_t channels, int64_t rows, bool two_digits, int pieces, bool may_split) {
+Choice cheapest_tile(const TileCost (&tiles)[7], int64_t channels, int64_t rows, bool two_digits, int pieces, bool may_split) {
     Choice best = {0, 1};
     double least = 0;
     const double steps = pieces;
-    for (int i = 0; i < (two_digits ? 5 : 6); ++i) {   // (two digits are two blocks of 16 rows)
+    for (int i = 0; i < (two_digits ? 6 : 7); ++i) {   // (two digits are two blocks of 16 rows)
         const int64_t across = (rows + tiles[i].tokens - 1) / tiles[i].tokens;
         const double n = static_cast<double>((channels + tiles[i].channels - 1) / tiles[i].channels) * static_cast<double>(across);
         const double alone = across == 1 ? 1.4 * tiles[i].alone : tiles[i].alone;
         const double rounds = n <= 256 ? n / 256 : std::ceil(n / 256);   // (256 compute units)
         const double cost = std::max(alone, rounds * tiles[i].share) * steps + std::max(1., rounds) * tiles[i].fixed;
         if (i == 0 || cost < least) best = {i, 1}, least = cost;
-        if (i < 4 || !may_split) continue;
+        if (i < 5 || !may_split) continue;
         const uint32_t splits = static_cast<uint32_t>(std::min({kI8SplitTiles / n, steps / 8, 16.}));
         if (splits < 2) continue;
         const double shared = std::max(alone, n * splits / 256 * tiles[i].share) * steps / splits + tiles[i].fixed + kJoin;
@@ -584,7 +586,10 @@ lordba_status product(ProductArgs a, hipStream_t stream) {
         case 1: return product_launch<256, 128, 4, 2, 1, 4, DIG, GATED>(a, stream);
         case 2: return product_launch<128, 128, 2, 4, 1, 4, DIG, GATED>(a, stream);
         case 3: return product_launch<64, 64, 1, 2, 2, 4, DIG, GATED>(a, stream);
-        case 4: return product_launch<GATED ? 64 : 32, 32, 1, 1, GATED ? 2 : 4, 4, DIG, GATED>(a, stream);
+        case 4:
+            if constexpr (!GATED) return product_launch<32, 64, 1, 2, 2, 4, DIG, GATED>(a, stream);
+            [[fallthrough]];
+        case 5: return product_launch<GATED ? 64 : 32, 32, 1, 1, GATED ? 2 : 4, 4, DIG, GATED>(a, stream);
         default:
             if constexpr (DIG == 1) return product_launch<GATED ? 64 : 32, 16, 1, 1, GATED ? 2 : 4, 4, DIG, GATED>(a, stream);
             return LORDBA_ERR_LAUNCH;   // (cheapest_tile does not name it)
