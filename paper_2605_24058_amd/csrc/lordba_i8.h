@@ -27,14 +27,15 @@ inline size_t i8_scale_offset(int64_t T, int64_t cols, int digits) {   // the ro
     return (static_cast<size_t>(digits) * static_cast<size_t>(T) * static_cast<size_t>(i8_row_bytes(cols)) + 255) / 256 * 256;
 }
 
-// Few rows of a long contraction: behind them lies room for the counters and the partial sums of kI8SplitTiles workgroups of 64 x 32 sums.
+// Few rows of a long contraction: behind them lies room for the counters and the partial sums of kI8SplitTiles workgroups of up to 64 x 64 sums
+// (a counter for each of the up to two waves that a tile's sums end in: only tiles that two workgroups or more share have them).
 constexpr int64_t kI8SplitColumns = 2048, kI8SplitRows = 512, kI8SplitTiles = 256;
 inline bool i8_splits(int64_t T, int64_t cols, int digits) { return i8_row_bytes(cols) >= kI8SplitColumns && T * digits <= kI8SplitRows; }
 inline size_t i8_split_offset(int64_t T, int64_t cols, int digits) {
     return (i8_scale_offset(T, cols, digits) + static_cast<size_t>(T) * 4 + 255) / 256 * 256;
 }
 inline size_t i8_workspace_bytes(int64_t T, int64_t cols, int digits) {
-    return i8_split_offset(T, cols, digits) + (i8_splits(T, cols, digits) ? kI8SplitTiles * (4 + 64 * 32 * 4) : 0);
+    return i8_split_offset(T, cols, digits) + (i8_splits(T, cols, digits) ? kI8SplitTiles * (4 + 64 * 64 * 4) : 0);
 }
 
 inline bool i8_overlap(const void* p, size_t pn, const void* q, size_t qn) {

@@ -270,7 +270,7 @@ __global__ __launch_bounds__(64 * WC * WT * WK) void lordba_i8_product_kernel(Pr
     const Tile tile = tile_of(a.first + blockIdx.x, static_cast<uint32_t>((a.n + kCols - 1) / kCols), static_cast<uint32_t>((a.T + kTokens - 1) / kTokens));
     const int64_t c0 = static_cast<int64_t>(tile.c) * kCols, t0 = static_cast<int64_t>(tile.t) * kTokens;
     // (SPLIT: this workgroup has the steps k0 .. k0 + K - 1 of the contraction)
-    constexpr bool SPLIT = WC * WT == 1 && WK > 1 && !OWN_ROWS;
+    constexpr bool SPLIT = WC * WT <= 2 && WK > 1 && !OWN_ROWS;
     const int steps = (a.pieces + WK - 1) / WK;
     const int k0 = SPLIT ? static_cast<int>(static_cast<int64_t>(steps) * blockIdx.y / a.splits) : 0;
     const int K = SPLIT ? static_cast<int>(static_cast<int64_t>(steps) * (blockIdx.y + 1) / a.splits) - k0 : steps;
@@ -432,11 +432,12 @@ __global__ __launch_bounds__(64 * WC * WT * WK) void lordba_i8_product_kernel(Pr
                 for (int j = 0; j < TB; ++j) acc[i][j] += sums[(p * WC * WT * CB * TB + i * TB + j) * 64];
     }
     if constexpr (SPLIT) {
-        // The last workgroup of a tile to arrive joins the parts: whole numbers, any order gives the same sum.  The parts go through the memory that all XCDs
+        // The last workgroup of a tile to arrive joins the parts (each of its waves its own blocks): whole numbers, any order gives the same sum.  The parts go through the memory that all XCDs
         // share, piece by piece (accesses of agent scope), not by a fence, which would have the XCD's whole L2 written back (3 us more).
         if (a.splits > 1) {
-            uint64_t* const parts = reinterpret_cast<uint64_t*>(a.parts) + static_cast<int64_t>(blockIdx.x) * (CB * TB * 128) + lane;
-            const int64_t apart = static_cast<int64_t>(gridDim.x) * (CB * TB * 128);
+            const uint32_t mine_of = blockIdx.x * (WC * WT) + wave % (WC * WT);
+            uint64_t* const parts = reinterpret_cast<uint64_t*>(a.parts) + static_cast<int64_t>(mine_of) * (CB * TB * 128) + lane;
+            const int64_t apart = static_cast<int64_t>(gridDim.x) * (WC * WT * CB * TB * 128);
             typedef uint64_t l2v __attribute__((ext_vector_type(2)));
 #pragma unroll
             for (int i = 0; i < CB * TB; ++i) {
@@ -446,7 +447,7 @@ __global__ __launch_bounds__(64 * WC * WT * WK) void lordba_i8_product_kernel(Pr
             }
             asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // (the parts are there before the arrival is counted)
             uint32_t before = 0;
-            if (lane == 0) before = __hip_atomic_fetch_add(a.arrived + blockIdx.x, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+            if (lane == 0) before = __hip_atomic_fetch_add(a.arrived + mine_of, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
             if (__builtin_amdgcn_readfirstlane(before) + 1 != a.splits) return;
             asm volatile("" ::: "memory");
             // several parts are on their way at a time: each way takes about a microsecond
@@ -538,7 +539,7 @@ lordba_status product_launch(const ProductArgs& a, hipStream_t stream) {
 }
 
 // The tiles and their times on a compute unit, in nanoseconds: a step of 64 columns alone on a chip with few workgroups (waiting; 1.4 times that where the
-// weights are read once, from memory), the same as a share of a chip that is full (throughput; small tiles run side by side on a unit), and what comes around
+// weights are read once or come from memory), the same as a share of a chip that is full (throughput; small tiles run side by side on a unit), and what comes around
 // the steps, filling and results.  Fitted to some forty shapes of 1 to 16384 rows, 64 to 13824 columns, even and odd; the tile with the least sum was the
 // fastest of the six or within 15 % of it on all but a few of them (6536 x 129 x 1910 gated: 26 us instead of 19).
 struct TileCost {
@@ -561,14 +562,15 @@ Choice cheapest_tile(const TileCost (&tiles)[7], int64_t channels, int64_t rows,
     Choice best = {0, 1};
     double least = 0;
     const double steps = pieces;
+    const bool from_memory = channels * pieces * 64 > (24 << 20);   // (weights that the caches of the XCDs do not hold)
     for (int i = 0; i < (two_digits ? 6 : 7); ++i) {   // (two digits are two blocks of 16 rows)
         const int64_t across = (rows + tiles[i].tokens - 1) / tiles[i].tokens;
         const double n = static_cast<double>((channels + tiles[i].channels - 1) / tiles[i].channels) * static_cast<double>(across);
-        const double alone = across == 1 ? 1.4 * tiles[i].alone : tiles[i].alone;
+        const double alone = across == 1 || from_memory ? 1.4 * tiles[i].alone : tiles[i].alone;
         const double rounds = n <= 256 ? n / 256 : std::ceil(n / 256);   // (256 compute units)
         const double cost = std::max(alone, rounds * tiles[i].share) * steps + std::max(1., rounds) * tiles[i].fixed;
         if (i == 0 || cost < least) best = {i, 1}, least = cost;
-        if (i < 5 || !may_split) continue;
+        if (i < 3 || !may_split) continue;
         const uint32_t splits = static_cast<uint32_t>(std::min({kI8SplitTiles / n, steps / 8, 16.}));
         if (splits < 2) continue;
         const double shared = std::max(alone, n * splits / 256 * tiles[i].share) * steps / splits + tiles[i].fixed + kJoin;
