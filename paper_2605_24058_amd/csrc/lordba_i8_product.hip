@@ -185,7 +185,8 @@ __device__ __forceinline__ Tile tile_of(uint32_t id, uint32_t nc, uint32_t nt) {
 }
 
 // A few tokens' rows brought to digits by the workgroup itself (OWN_ROWS): x comes into LDS the way of the weights, ahead of them, and its 8-bit rows are
-// kept there.  Behind the ring: x, rows of whole KiB; the rows, a.ld bytes each; their scales.
+// kept there.  Behind the ring: x, rows of whole KiB; the rows, a.ld bytes each; their scales.  OWN_ROWS = 2: rows that do not consist of aligned 16-byte
+// pieces are read through registers, twice, behind the weights that have been requested (loads return in order).
 __host__ __device__ __forceinline__ int64_t own_x_bytes(int64_t d_in) { return (d_in * 2 + 1023) / 1024 * 1024; }
 __host__ __device__ __forceinline__ int64_t own_bytes(int64_t T, int64_t d_in, int64_t ld) { return T * (own_x_bytes(d_in) + ld) + 64 * 4 * 2; }
 __device__ __forceinline__ int8_t* own_rows_at(const ProductArgs& a, int8_t* lds) { return lds + a.T * own_x_bytes(a.d_in); }
@@ -203,21 +204,26 @@ __device__ __forceinline__ void own_rows_request(const ProductArgs& a, int8_t* l
 }
 
 // LATER: loads that this wave has requested since
-template <int THREADS, int LATER>
+template <int THREADS, int LATER, bool PIECES>
 __device__ __forceinline__ void own_rows(const ProductArgs& a, int8_t* lds) {
     const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
     int8_t* const rows = own_rows_at(a, lds);
     float* const scales = own_scales_at(a, lds);
     uint32_t* const part = reinterpret_cast<uint32_t*>(scales + 16);   // [token][wave]
-    asm volatile("s_waitcnt vmcnt(%0)" :: "n"(LATER) : "memory");
-    __builtin_amdgcn_s_barrier();
-    asm volatile("" ::: "memory");
-    const uint32_t groups = static_cast<uint32_t>(a.d_in / 8), all = static_cast<uint32_t>(a.ld / 8);
+    if constexpr (PIECES) {
+        asm volatile("s_waitcnt vmcnt(%0)" :: "n"(LATER) : "memory");
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+    }
+    const uint32_t groups = static_cast<uint32_t>((a.d_in + 7) / 8), all = static_cast<uint32_t>(a.ld / 8);
+    auto group_of = [&](int t, uint32_t k) {
+        if constexpr (PIECES) return reinterpret_cast<const u4*>(lds + t * own_x_bytes(a.d_in))[k];
+        else return load_part(a.x + t * a.d_in, 8 * static_cast<int64_t>(k), a.d_in);
+    };
     for (int t = 0; t < a.T; ++t) {
-        const u4* const x = reinterpret_cast<const u4*>(lds + t * own_x_bytes(a.d_in));
         uint32_t m = 0;   // (fp16 magnitudes as unsigned numbers, a NaN the largest)
         for (uint32_t k = threadIdx.x; k < groups; k += THREADS) {
-            const u4 v = x[k];
+            const u4 v = group_of(t, k);
 #pragma unroll
             for (int e = 0; e < 4; ++e) m = max(m, max(v[e] & 0x7FFFu, v[e] >> 16 & 0x7FFFu));
         }
@@ -229,14 +235,13 @@ __device__ __forceinline__ void own_rows(const ProductArgs& a, int8_t* lds) {
     __builtin_amdgcn_s_barrier();
     asm volatile("" ::: "memory");
     for (int t = 0; t < a.T; ++t) {
-        const u4* const x = reinterpret_cast<const u4*>(lds + t * own_x_bytes(a.d_in));
         uint32_t m = part[t * (THREADS / 64)];
 #pragma unroll
         for (int w = 1; w < THREADS / 64; ++w) m = max(m, part[t * (THREADS / 64) + w]);
         const RowScale s = scale_of(__float_as_uint(static_cast<float>(__builtin_bit_cast(_Float16, static_cast<uint16_t>(m)))), 127.f);
         if (threadIdx.x == 0) scales[t] = s.scale;
         for (uint32_t k = threadIdx.x; k < all; k += THREADS) {
-            const h8 h = as_h8(k < groups ? x[k] : u4{0u, 0u, 0u, 0u});
+            const h8 h = as_h8(k < groups ? group_of(t, k) : u4{0u, 0u, 0u, 0u});
             float f[8];
 #pragma unroll
             for (int e = 0; e < 8; ++e) f[e] = static_cast<float>(h[e]);
@@ -258,7 +263,7 @@ __device__ __forceinline__ void own_rows(const ProductArgs& a, int8_t* lds) {
 // the lane, so it is the lane's address that is permuted.
 // While a step's products run on one set of operand registers, the next step's operands are read into the other.
 // The barrier of step k says that step k + 1 has landed and that everybody has read step k, whose slot then takes step k + S.
-template <int CT, int TT, int WC, int WT, int WK, int S, int DIG, bool GATED, bool OWN_ROWS = false>
+template <int CT, int TT, int WC, int WT, int WK, int S, int DIG, bool GATED, int OWN_ROWS = 0>
 __global__ __launch_bounds__(64 * WC * WT * WK) void lordba_i8_product_kernel(ProductArgs a) {
     constexpr int NW = WC * WT * WK, CB = CT / 16 / WC, TB = TT / 16 / WT, NB = (OWN_ROWS ? CT : CT + TT) / 16, L = NB * WK / NW;
     constexpr uint32_t kPart = NB * 1024u, kSlot = WK * kPart;
@@ -292,17 +297,17 @@ __global__ __launch_bounds__(64 * WC * WT * WK) void lordba_i8_product_kernel(Pr
         }
         to = to + kSlot == to_end ? to_end - S * kSlot : to + kSlot;
     };
-    if constexpr (OWN_ROWS) {
+    if constexpr (OWN_ROWS != 0) {
         static_assert(DIG == 1 && TT == 16 && WC == 1 && WT == 1, "one block of tokens, read by every wave");
-        own_rows_request<64 * NW>(a, lds + S * kSlot);
+        if constexpr (OWN_ROWS == 1) own_rows_request<64 * NW>(a, lds + S * kSlot);
     }
 #pragma unroll
     for (int k = 0; k < S; ++k)
         if (k < K) request();
     const int8_t* own = nullptr;
-    if constexpr (OWN_ROWS) {
-        if (K >= S) own_rows<64 * NW, S * L>(a, lds + S * kSlot);
-        else own_rows<64 * NW, 0>(a, lds + S * kSlot);
+    if constexpr (OWN_ROWS != 0) {
+        if (K >= S) own_rows<64 * NW, S * L, OWN_ROWS == 1>(a, lds + S * kSlot);
+        else own_rows<64 * NW, 0, OWN_ROWS == 1>(a, lds + S * kSlot);
         own = own_rows_at(a, lds + S * kSlot) + min<int64_t>(lane & 15, a.T - 1) * a.ld + 64 * wk + 16 * (lane >> 4);
         a.q_scale = own_scales_at(a, lds + S * kSlot);
     }
@@ -318,7 +323,7 @@ __global__ __launch_bounds__(64 * WC * WT * WK) void lordba_i8_product_kernel(Pr
     auto read = [&](auto set) {
 #pragma unroll
         for (int i = 0; i < CB; ++i) fc[set.value][i] = *reinterpret_cast<const i4*>(at_c + from + i * 1024);
-        if constexpr (OWN_ROWS) {
+        if constexpr (OWN_ROWS != 0) {
             ft[set.value][0] = *reinterpret_cast<const i4*>(own);
             if ((lane & 15) >= a.T) ft[set.value][0] = i4{0, 0, 0, 0};
             own += 64 * WK;
@@ -505,7 +510,7 @@ __global__ __launch_bounds__(64 * WC * WT * WK) void lordba_i8_product_kernel(Pr
 
 constexpr size_t kLdsBytes = 160 * 1024;
 
-template <int CT, int TT, int WC, int WT, int WK, int S, int DIG, bool GATED, bool OWN_ROWS = false>
+template <int CT, int TT, int WC, int WT, int WK, int S, int DIG, bool GATED, int OWN_ROWS = 0>
 lordba_status product_launch(const ProductArgs& a, hipStream_t stream) {
     constexpr int kCols = GATED ? CT / 2 : CT, kTokens = TT / DIG;
     constexpr size_t kRing = S * WK * (OWN_ROWS ? CT : CT + TT) * 64;
@@ -602,10 +607,21 @@ lordba_status product(ProductArgs a, hipStream_t stream) {
 // call in us, with the row kernel -> without, T x d_in -> d_out: 1 x 4096 -> 4096 7.9 -> 5.8, 1 x 4096 -> 11008 12.2 -> 8.9, 1 x 11008 -> 4096 13.2 -> 11.7,
 // 2 x 4096 -> 4096 8.0 -> 6.8, 2 x 11008 -> 4096 13.1 -> 13.6, 4 x 1000 -> 1024 8.2 -> 5.9, 4 x 4096 -> 11008 12.4 -> 17.8, 16 x 512 -> 512 8.5 -> 12.9 (tokens are
 // taken one after the other); gated, 1 x 4096 x 11008 19.6 -> 17.2, 2 x 4096 x 11008 19.4 -> 21.9.
+// Rows read through registers cost more: 1 x 126 -> 292 8.5 -> 5.1, 1 x 566 x 286 gated 8.4 -> 5.4, but 2 x 4095 -> 4096 8.5 either way, 1 x 13823 -> 4096 13.9 -> 15.0,
+// 4 x 1001 -> 1024 7.8 -> 8.3.
+bool own_pieces(const ProductArgs& a) { return a.d_in % 8 == 0 && !i8_misaligned(a.x, 16); }
+
 template <bool GATED>
 bool own_rows_fit(const ProductArgs& a, int digits) {
-    return digits == 1 && a.T <= 4 && a.T * a.d_in <= (GATED ? 6144 : 14336) && a.d_in % 8 == 0 && !i8_misaligned(a.x, 16) &&
+    const int64_t most = own_pieces(a) ? (GATED ? 6144 : 14336) : (GATED ? 2048 : 4096);
+    return digits == 1 && a.T <= (own_pieces(a) ? 4 : 2) && a.T * a.d_in <= most &&
            static_cast<size_t>(own_bytes(a.T, a.d_in, a.ld)) + 4 * 4 * (GATED ? 64 : 32) * 64 <= kLdsBytes;
+}
+
+template <bool GATED>
+lordba_status own_rows_product(const ProductArgs& a, hipStream_t stream) {
+    if (own_pieces(a)) return product_launch<GATED ? 64 : 32, 16, 1, 1, 4, 4, 1, GATED, 1>(a, stream);
+    return product_launch<GATED ? 64 : 32, 16, 1, 1, 4, 4, 1, GATED, 2>(a, stream);
 }
 
 // What the four entry points check alike.
@@ -664,7 +680,7 @@ lordba_status linear(const void* x, const float* col_scale, const int8_t* w, con
     const Workspace ws = split(workspace, T, contracted, digits);
     const ProductArgs a = {w, ws.q, ws.scale, w_scale, nullptr, static_cast<_Float16*>(y), nullptr, T, n, i8_row_bytes(contracted), static_cast<int>((contracted + 63) / 64),
                            static_cast<const _Float16*>(x), contracted, ws.parts, ws.arrived, 1, 0};
-    if (!col_scale && own_rows_fit<false>(a, digits)) return product_launch<32, 16, 1, 1, 4, 4, 1, false, true>(a, st);
+    if (!col_scale && own_rows_fit<false>(a, digits)) return own_rows_product<false>(a, st);
     const lordba_status rows = lordba_i8_quantize(x, col_scale, ws.q, ws.scale, split_arrivals(ws, T, contracted, digits), T, contracted, digits, st);
     if (rows != LORDBA_OK) return rows;
     return digits == 1 ? product<1, false>(a, st) : product<2, false>(a, st);
@@ -705,7 +721,7 @@ extern "C" lordba_status lordba_gated_i8(const void* x, const int8_t* W, const f
     const Workspace ws = split(workspace, T, d_in, digits);
     const ProductArgs a = {W, ws.q, ws.scale, w_scale, static_cast<const _Float16*>(addends), static_cast<_Float16*>(h), static_cast<_Float16*>(gate_up),
                            T, d_ff, i8_row_bytes(d_in), static_cast<int>((d_in + 63) / 64), static_cast<const _Float16*>(x), d_in, ws.parts, ws.arrived, 1, 0};
-    if (own_rows_fit<true>(a, digits)) return product_launch<64, 16, 1, 1, 4, 4, 1, true, true>(a, s);
+    if (own_rows_fit<true>(a, digits)) return own_rows_product<true>(a, s);
     if ((st = lordba_i8_quantize(x, nullptr, ws.q, ws.scale, split_arrivals(ws, T, d_in, digits), T, d_in, digits, s)) != LORDBA_OK) return st;
     return digits == 1 ? product<1, true>(a, s) : product<2, true>(a, s);
 }

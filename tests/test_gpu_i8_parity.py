@@ -178,7 +178,8 @@ def test_linear_backward(torch, shape, digits):
 # or columns, long contractions), and a few tokens whose rows the product's workgroups make (multiples of 8 columns, 16-byte aligned)
 REGIMES = [(2100, 300, 4200), (2048, 520, 4095), (1030, 260, 4100), (512, 700, 4096), (600, 250, 1111), (40, 5000, 70), (3, 9000, 40), (16, 131071, 3), (20, 3000, 33),
            (130, 2100, 20), (1, 4096, 515), (2, 6000, 100), (7, 1024, 64), (1, 13824, 33), (3, 4104, 37), (16, 64, 8), (16, 880, 31), (158, 34321, 771),
-           (237, 37461, 34), (113, 27294, 500), (165, 14105, 68), (64, 13824, 2100), (128, 2600, 4096), (60, 2000, 3500)]
+           (237, 37461, 34), (113, 27294, 500), (165, 14105, 68), (64, 13824, 2100), (128, 2600, 4096), (60, 2000, 3500),
+           (1, 4095, 300), (2, 2047, 65), (1, 9, 40), (2, 1, 33)]
 
 
 @pytest.mark.parametrize("digits", [1, 2])
@@ -197,7 +198,8 @@ def test_linear_regimes(torch, shape, digits):
 
 
 @pytest.mark.parametrize("shape", [(2053, 320, 4096), (2048, 256, 4090), (1024, 300, 3001), (512, 260, 2048), (4, 6000, 30), (20, 3000, 17), (1, 4096, 100), (3, 2048, 50),
-                                   (1, 6144, 9), (267, 20889, 85), (17, 14034, 400), (114, 9500, 282), (700, 500, 640)], ids=lambda s: "T%d_%dx%d" % s)
+                                   (1, 6144, 9), (267, 20889, 85), (17, 14034, 400), (114, 9500, 282), (700, 500, 640),
+                                   (1, 2047, 70), (2, 1001, 33)], ids=lambda s: "T%d_%dx%d" % s)
 def test_gated_regimes(torch, shape):
     T, d_in, F = shape
     rng = np.random.default_rng(T + 31 * d_in + 37 * F)
