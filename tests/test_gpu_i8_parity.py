@@ -418,9 +418,9 @@ def test_more_rows_than_a_launch(torch):
     near(host(many)[0], gated_loss_parts(d, gate, up)[0], np.abs(d * up) * 2.0 ** -17 * (1 + np.abs(gate)))
 
 
-def test_streams_and_graphs(torch):
+@pytest.mark.parametrize("T,d_in,F", [(50, 300, 90), (2100, 260, 2100), (60, 9000, 40), (2, 512, 64)])
+def test_streams_and_graphs(torch, T, d_in, F):
     rng = np.random.default_rng(6)
-    T, d_in, F = 50, 300, 90
     W, ws = weights(rng, 2 * F, d_in)
     w, sd = torch.from_numpy(W).cuda(), torch.from_numpy(ws).cuda()
     Wl, Wt = binding.lordba_layout_i8(w), binding.lordba_layout_i8(w, True)
@@ -435,10 +435,10 @@ def test_streams_and_graphs(torch):
     want = step()
     torch.cuda.synchronize()
     side = torch.cuda.Stream()
-    for stream in (side, side.cuda_stream):
+    for stream in (side, side.cuda_stream, 0):
         side.wait_stream(torch.cuda.current_stream())
         got = step(stream)
-        side.synchronize()
+        torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(got, want))
     graph = torch.cuda.CUDAGraph()
     with torch.cuda.graph(graph):
