@@ -44,10 +44,11 @@ inline bool i8_overlap(const void* p, size_t pn, const void* q, size_t qn) {
 }
 inline bool i8_misaligned(const void* p, uintptr_t bytes) { return (reinterpret_cast<uintptr_t>(p) & (bytes - 1)) != 0; }
 
-// Eight numbers of a row from column c < cols on, zeros from column `cols` on.  At a row's end all of them are requested before the first is
-// looked at: one wait, not eight.
+// Eight numbers of a row from column c < cols on, zeros from column `cols` on.  At a row's end the row's last eight are read and moved down: one
+// load, no entry by itself.  Rows of fewer than eight: all requested before the first is looked at.
 __device__ __forceinline__ u4 load_part(const _Float16* row, int64_t c, int64_t cols) {
     if (c + 8 <= cols) return load16_any(row + c);
+    if (cols >= 8) return drop_halves(load16_any(row + cols - 8), static_cast<int>(c + 8 - cols));
     uint32_t h[8];
 #pragma unroll
     for (int e = 0; e < 8; ++e) h[e] = reinterpret_cast<const uint16_t*>(row)[min(c + e, cols - 1)];
