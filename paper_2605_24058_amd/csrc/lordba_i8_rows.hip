@@ -275,8 +275,8 @@ lordba_status gated_grad_launch(GatedGradArgs a, hipStream_t stream) {
 }
 
 // With many rows of up to 1024 columns a wave has a row of its own (16384 x 320: 58 -> 27 us for the call); few rows are done sooner by more waves (190 x 811
-// 8.7 -> 5.8 us).  (1024 threads of two groups each, for the longest rows, spilled:
-// 72 us instead of 62 at 2048 x 11008.)
+// 8.7 -> 5.8 us, both with row ends stored entry by entry; 4.3 since).  (1024 threads of two groups each, for the longest rows, spilled: 72 us instead of 62 at
+// 2048 x 11008.)
 template <int DIG>
 lordba_status gated_grad(const GatedGradArgs& a, hipStream_t stream) {
     const bool many = a.T >= 512;
