@@ -16,21 +16,14 @@
 #include "lordba.h"
 #include "lordba_dev_util.h"
 #include "lordba_host_util.h"
+#include "lordba_i8_choice.h"
 
 namespace {
-
-constexpr int64_t kI8Step = 256;   // columns that a row is padded to: up to four waves share a step of 64 each
-
-inline int64_t i8_row_bytes(int64_t cols) { return (cols + kI8Step - 1) / kI8Step * kI8Step; }
 
 inline size_t i8_scale_offset(int64_t T, int64_t cols, int digits) {   // the rows' scales lie behind the rows in a workspace
     return (static_cast<size_t>(digits) * static_cast<size_t>(T) * static_cast<size_t>(i8_row_bytes(cols)) + 255) / 256 * 256;
 }
 
-// Few rows of a long contraction: behind them lies room for the counters and the partial sums of kI8SplitTiles workgroups of up to 64 x 64 sums
-// (a counter for each of the up to two waves that a tile's sums end in: only tiles that two workgroups or more share have them).
-constexpr int64_t kI8SplitColumns = 2048, kI8SplitRows = 512, kI8SplitTiles = 256;
-inline bool i8_splits(int64_t T, int64_t cols, int digits) { return i8_row_bytes(cols) >= kI8SplitColumns && T * digits <= kI8SplitRows; }
 inline size_t i8_split_offset(int64_t T, int64_t cols, int digits) {
     return (i8_scale_offset(T, cols, digits) + static_cast<size_t>(T) * 4 + 255) / 256 * 256;
 }

@@ -6,7 +6,6 @@
 // factors of its outputs.
 #include <algorithm>
 #include <atomic>
-#include <cmath>
 #include <type_traits>
 
 #include "lordba_dev_util.h"
@@ -187,8 +186,6 @@ __device__ __forceinline__ Tile tile_of(uint32_t id, uint32_t nc, uint32_t nt) {
 // A few tokens' rows brought to digits by the workgroup itself (OWN_ROWS): x comes into LDS the way of the weights, ahead of them, and its 8-bit rows are
 // kept there.  Behind the ring: x, rows of whole KiB; the rows, a.ld bytes each; their scales.  OWN_ROWS = 2: rows that do not consist of aligned 16-byte
 // pieces are read through registers, twice, behind the weights that have been requested (loads return in order).
-__host__ __device__ __forceinline__ int64_t own_x_bytes(int64_t d_in) { return (d_in * 2 + 1023) / 1024 * 1024; }
-__host__ __device__ __forceinline__ int64_t own_bytes(int64_t T, int64_t d_in, int64_t ld) { return T * (own_x_bytes(d_in) + ld) + 64 * 4 * 2; }
 __device__ __forceinline__ int8_t* own_rows_at(const ProductArgs& a, int8_t* lds) { return lds + a.T * own_x_bytes(a.d_in); }
 __device__ __forceinline__ float* own_scales_at(const ProductArgs& a, int8_t* lds) { return reinterpret_cast<float*>(own_rows_at(a, lds) + a.T * a.ld); }
 
@@ -508,8 +505,6 @@ __global__ __launch_bounds__(64 * WC * WT * WK) void lordba_i8_product_kernel(Pr
     finish_tile(from_memory);
 }
 
-constexpr size_t kLdsBytes = 160 * 1024;
-
 template <int CT, int TT, int WC, int WT, int WK, int S, int DIG, bool GATED, int OWN_ROWS = 0>
 lordba_status product_launch(const ProductArgs& a, hipStream_t stream) {
     constexpr int kCols = GATED ? CT / 2 : CT, kTokens = TT / DIG;
@@ -543,50 +538,9 @@ lordba_status product_launch(const ProductArgs& a, hipStream_t stream) {
     return LORDBA_OK;
 }
 
-// The tiles and their times on a compute unit, in nanoseconds: a step of 64 columns alone on a chip with few workgroups (waiting; 1.4 times that where the
-// weights are read once or come from memory), the same as a share of a chip that is full (throughput; small tiles run side by side on a unit), and what comes around
-// the steps, filling and results.  Fitted to some forty shapes of 1 to 16384 rows, 64 to 13824 columns, even and odd; the tile with the least sum was the
-// fastest of the six or within 15 % of it on all but a few of them (6536 x 129 x 1910 gated: 26 us instead of 19).
-struct TileCost {
-    int channels, tokens;
-    double alone, share, fixed;
-};
-constexpr TileCost kTiles[7] = {{256, 256, 600, 800, 7000}, {256, 128, 390, 510, 3400}, {128, 128, 200, 300, 1100}, {64, 64, 77, 125, 600},
-                                {32, 64, 55, 80, 400},      {32, 32, 35, 60, 300},      {32, 16, 25, 50, 300}};
-constexpr TileCost kGatedTiles[7] = {{256, 256, 600, 800, 18000}, {256, 128, 390, 510, 9500}, {128, 128, 200, 300, 5000}, {64, 64, 77, 125, 1500},
-                                     {64, 32, 60, 105, 1000},     {64, 32, 60, 105, 1000},    {64, 16, 40, 100, 600}};   // (64 x 32 stands for both small plain ones)
-
-// Few small tiles of a long contraction: several workgroups share a tile's steps, which costs them kJoin ns to join (the product of 4 x 25742 -> 83 in two
-// digits 15.8 -> 6.4 us).
-constexpr double kJoin = 6000;
-struct Choice {
-    int tile;
-    uint32_t splits;
-};
-Choice cheapest_tile(const TileCost (&tiles)[7], int64_t channels, int64_t rows, bool two_digits, int pieces, bool may_split) {
-    Choice best = {0, 1};
-    double least = 0;
-    const double steps = pieces;
-    const bool from_memory = channels * pieces * 64 > (24 << 20);   // (weights that the caches of the XCDs do not hold)
-    for (int i = 0; i < (two_digits ? 6 : 7); ++i) {   // (two digits are two blocks of 16 rows)
-        const int64_t across = (rows + tiles[i].tokens - 1) / tiles[i].tokens;
-        const double n = static_cast<double>((channels + tiles[i].channels - 1) / tiles[i].channels) * static_cast<double>(across);
-        const double alone = across == 1 || from_memory ? 1.4 * tiles[i].alone : tiles[i].alone;
-        const double rounds = n <= 256 ? n / 256 : std::ceil(n / 256);   // (256 compute units)
-        const double cost = std::max(alone, rounds * tiles[i].share) * steps + std::max(1., rounds) * tiles[i].fixed;
-        if (i == 0 || cost < least) best = {i, 1}, least = cost;
-        if (i < 3 || !may_split) continue;
-        const uint32_t splits = static_cast<uint32_t>(std::min({kI8SplitTiles / n, steps / 8, 16.}));
-        if (splits < 2) continue;
-        const double shared = std::max(alone, n * splits / 256 * tiles[i].share) * steps / splits + tiles[i].fixed + kJoin;
-        if (shared < least) best = {i, splits}, least = shared;
-    }
-    return best;
-}
-
 template <int DIG, bool GATED>
 lordba_status product(ProductArgs a, hipStream_t stream) {
-    const Choice choice = cheapest_tile(GATED ? kGatedTiles : kTiles, (GATED ? 2 : 1) * a.n, DIG * a.T, DIG == 2, a.pieces, i8_splits(a.T, a.ld, DIG));
+    const Choice choice = i8_choice(a.T, 64 * static_cast<int64_t>(a.pieces), a.n, DIG, GATED);
     a.splits = choice.splits;
     switch (choice.tile) {
         case 0: return product_launch<256, 256, 4, 2, 1, 4, DIG, GATED>(a, stream);
@@ -603,24 +557,9 @@ lordba_status product(ProductArgs a, hipStream_t stream) {
     }
 }
 
-// Whether the product's workgroups bring the rows to digits themselves: one launch instead of two, but every workgroup does the whole of it.  Times of a
-// call in us, with the row kernel -> without, T x d_in -> d_out: 1 x 4096 -> 4096 7.9 -> 5.8, 1 x 4096 -> 11008 12.2 -> 8.9, 1 x 11008 -> 4096 13.2 -> 11.7,
-// 2 x 4096 -> 4096 8.0 -> 6.8, 2 x 11008 -> 4096 13.1 -> 13.6, 4 x 1000 -> 1024 8.2 -> 5.9, 4 x 4096 -> 11008 12.4 -> 17.8, 16 x 512 -> 512 8.5 -> 12.9 (tokens are
-// taken one after the other); gated, 1 x 4096 x 11008 19.6 -> 17.2, 2 x 4096 x 11008 19.4 -> 21.9.
-// Rows read through registers cost more: 1 x 126 -> 292 8.5 -> 5.1, 1 x 566 x 286 gated 8.4 -> 5.4, but 2 x 4095 -> 4096 8.5 either way, 1 x 13823 -> 4096 13.9 -> 15.0,
-// 4 x 1001 -> 1024 7.8 -> 8.3.
-bool own_pieces(const ProductArgs& a) { return a.d_in % 8 == 0 && !i8_misaligned(a.x, 16); }
-
 template <bool GATED>
-bool own_rows_fit(const ProductArgs& a, int digits) {
-    const int64_t most = own_pieces(a) ? (GATED ? 6144 : 14336) : (GATED ? 2048 : 4096);
-    return digits == 1 && a.T <= (own_pieces(a) ? 4 : 2) && a.T * a.d_in <= most &&
-           static_cast<size_t>(own_bytes(a.T, a.d_in, a.ld)) + 4 * 4 * (GATED ? 64 : 32) * 64 <= kLdsBytes;
-}
-
-template <bool GATED>
-lordba_status own_rows_product(const ProductArgs& a, hipStream_t stream) {
-    if (own_pieces(a)) return product_launch<GATED ? 64 : 32, 16, 1, 1, 4, 4, 1, GATED, 1>(a, stream);
+lordba_status own_rows_product(const ProductArgs& a, int from, hipStream_t stream) {
+    if (from == 1) return product_launch<GATED ? 64 : 32, 16, 1, 1, 4, 4, 1, GATED, 1>(a, stream);
     return product_launch<GATED ? 64 : 32, 16, 1, 1, 4, 4, 1, GATED, 2>(a, stream);
 }
 
@@ -678,9 +617,9 @@ lordba_status linear(const void* x, const float* col_scale, const int8_t* w, con
     if (dev != LORDBA_OK) return dev;
     const hipStream_t st = static_cast<hipStream_t>(stream);
     const Workspace ws = split(workspace, T, contracted, digits);
-    const ProductArgs a = {w, ws.q, ws.scale, w_scale, nullptr, static_cast<_Float16*>(y), nullptr, T, n, i8_row_bytes(contracted), static_cast<int>((contracted + 63) / 64),
+    const ProductArgs a = {w, ws.q, ws.scale, w_scale, nullptr, static_cast<_Float16*>(y), nullptr, T, n, i8_row_bytes(contracted), static_cast<int>(i8_pieces(contracted)),
                            static_cast<const _Float16*>(x), contracted, ws.parts, ws.arrived, 1, 0};
-    if (!col_scale && own_rows_fit<false>(a, digits)) return own_rows_product<false>(a, st);
+    if (const int own = col_scale ? 0 : i8_own_rows(T, contracted, digits, false, !i8_misaligned(x, 16))) return own_rows_product<false>(a, own, st);
     const lordba_status rows = lordba_i8_quantize(x, col_scale, ws.q, ws.scale, split_arrivals(ws, T, contracted, digits), T, contracted, digits, st);
     if (rows != LORDBA_OK) return rows;
     return digits == 1 ? product<1, false>(a, st) : product<2, false>(a, st);
@@ -720,8 +659,8 @@ extern "C" lordba_status lordba_gated_i8(const void* x, const int8_t* W, const f
     const hipStream_t s = static_cast<hipStream_t>(stream);
     const Workspace ws = split(workspace, T, d_in, digits);
     const ProductArgs a = {W, ws.q, ws.scale, w_scale, static_cast<const _Float16*>(addends), static_cast<_Float16*>(h), static_cast<_Float16*>(gate_up),
-                           T, d_ff, i8_row_bytes(d_in), static_cast<int>((d_in + 63) / 64), static_cast<const _Float16*>(x), d_in, ws.parts, ws.arrived, 1, 0};
-    if (own_rows_fit<true>(a, digits)) return own_rows_product<true>(a, s);
+                           T, d_ff, i8_row_bytes(d_in), static_cast<int>(i8_pieces(d_in)), static_cast<const _Float16*>(x), d_in, ws.parts, ws.arrived, 1, 0};
+    if (const int own = i8_own_rows(T, d_in, digits, true, !i8_misaligned(x, 16))) return own_rows_product<true>(a, own, s);
     if ((st = lordba_i8_quantize(x, nullptr, ws.q, ws.scale, split_arrivals(ws, T, d_in, digits), T, d_in, digits, s)) != LORDBA_OK) return st;
     return digits == 1 ? product<1, true>(a, s) : product<2, true>(a, s);
 }
@@ -744,6 +683,6 @@ extern "C" lordba_status lordba_gated_i8_backward(const void* dh, const void* ga
     const hipStream_t s = static_cast<hipStream_t>(stream);
     const Workspace ws = split(workspace, T, 2 * d_ff, digits);
     if ((st = lordba_i8_gated_grad(dh, gate_up, w_scale, dgate_up, ws.q, ws.scale, split_arrivals(ws, T, 2 * d_ff, digits), T, d_ff, digits, s)) != LORDBA_OK) return st;
-    const ProductArgs a = {Wt, ws.q, ws.scale, nullptr, nullptr, static_cast<_Float16*>(dx), nullptr, T, d_in, i8_row_bytes(2 * d_ff), static_cast<int>((2 * d_ff + 63) / 64), nullptr, 0, ws.parts, ws.arrived, 1, 0};
+    const ProductArgs a = {Wt, ws.q, ws.scale, nullptr, nullptr, static_cast<_Float16*>(dx), nullptr, T, d_in, i8_row_bytes(2 * d_ff), static_cast<int>(i8_pieces(2 * d_ff)), nullptr, 0, ws.parts, ws.arrived, 1, 0};
     return digits == 1 ? product<1, false>(a, s) : product<2, false>(a, s);
 }

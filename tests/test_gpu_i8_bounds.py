@@ -66,7 +66,7 @@ def ids(s):
     return "T%d_%dx%d" % s
 
 
-SHIFTS = (0, 1)     # elements behind 64 aligned bytes; matrices of bytes 16 of them
+SHIFTS = (0, 1)     # elements behind 64 aligned bytes; matrices of int8 16 of them
 
 
 @pytest.mark.gpu
@@ -123,7 +123,7 @@ def test_gated(torch, shape, digits):
 
 
 def check_gated(torch, T, d_in, F, digits, shifts=SHIFTS, ways=((True, True), (False, True), (True, False), (False, False))):
-    """ways: (with addends, kept) of the calls"""
+    """ways: (with addends, kept) of the calls; a shift of its own for the outputs where it is a pair"""
     rng = np.random.default_rng(T + 17 * d_in + 3 * F)
     W, ws = c.weights(rng, 2 * F, d_in)
     ws = (ws * 2).astype(np.float32)
@@ -135,8 +135,9 @@ def check_gated(torch, T, d_in, F, digits, shifts=SHIFTS, ways=((True, True), (F
         for keep in [k for a, k in ways if a == add]:
             for shift in shifts:
                 mem = c.Memory(torch)
-                got = mem.output((T, F), torch.float16, shift)
-                kept = mem.output((2, T, F), torch.float16, shift) if keep else None
+                shift, out = shift if isinstance(shift, tuple) else (shift, shift)
+                got = mem.output((T, F), torch.float16, out)
+                kept = mem.output((2, T, F), torch.float16, out) if keep else None
                 space = c.workspace(mem, T, d_in, digits)
                 call(torch, "lordba_gated_i8", mem.input(x, shift), mem.input(c.binding.lordba_layout_i8(w), 16 * shift), mem.input(ws, shift),
                      mem.input(addends, shift) if add else None, got, kept, space, space.numel(), T, d_in, F, digits)
