@@ -418,7 +418,10 @@ lordba_status lordba_ptq_beta_solve(const double* G, const double* h, double* be
 /* Bytes from one row to the next of a laid-out int8 matrix (0 for cols outside 1 .. LORDBA_I8_MAX_COLUMNS). */
 size_t lordba_i8_row_bytes(int64_t cols);
 
-/* Bytes of workspace for T rows of `cols` numbers in 1 or 2 digits (0 for arguments out of range). */
+/* Bytes of workspace for T rows of `cols` numbers in 1 or 2 digits (0 for arguments out of range).  Few rows of a long contraction have room for
+ * partial sums in it, which longer batches do not need: a workspace of the size for T serves every shorter batch, and fewer digits, too, but a
+ * contraction that would then be shared by several workgroups is not where that room is missing (the same results, in more time; the largest
+ * of the sizes of all lengths that a program runs avoids it). */
 size_t lordba_i8_workspace_bytes(int64_t T, int64_t cols, int digits);
 
 /* DEVICE function: lays out the plain row-major int8 matrix w [rows, cols] as [rows, lordba_i8_row_bytes(cols)], or, transposed != 0, its
@@ -435,7 +438,8 @@ lordba_status lordba_quantize_rows(const void* x, const float* col_scale, int8_t
 
 /* DEVICE function: y = x W^T by the definition above.
  *   x fp16 [T, d_in]; W laid-out int8 [d_out, .]; w_scale fp32 [d_out]; y fp16 [T, d_out] (out)
- *   workspace: lordba_i8_workspace_bytes(T, d_in, digits) bytes, 16-byte aligned, contents irrelevant; smaller -> LORDBA_ERR_WORKSPACE.
+ *   workspace: lordba_i8_workspace_bytes(T, d_in, digits) bytes, or those of a longer batch, 16-byte aligned, contents irrelevant; one too small for the
+ *   rows' integers and scales -> LORDBA_ERR_WORKSPACE.
  *   Calls that share a workspace must not overlap in time.
  * Any T >= 0 (0: no work), 1 <= d_in <= LORDBA_I8_MAX_COLUMNS, 1 <= d_out <= 2^24; activations aligned to their elements.  The call
  * only enqueues kernels on `stream`; it never synchronises, allocates or frees.  No output nor the workspace may overlap an input or

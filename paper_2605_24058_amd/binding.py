@@ -841,7 +841,8 @@ def lordba_i8_row_bytes(cols: int) -> int:
 
 
 def lordba_i8_workspace_bytes(T: int, cols: int, digits: int = 1) -> int:
-    """Bytes of workspace for T rows of `cols` numbers: d_in of the forward calls, d_out (2 d_ff) of the backward calls."""
+    """Bytes of workspace for T rows of `cols` numbers: d_in of the forward calls, d_out (2 d_ff) of the backward calls.  A workspace for the longest
+    batch serves shorter ones too."""
     return int(load_library().lordba_i8_workspace_bytes(T, cols, digits))
 
 

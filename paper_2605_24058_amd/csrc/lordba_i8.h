@@ -27,6 +27,9 @@ inline size_t i8_scale_offset(int64_t T, int64_t cols, int digits) {   // the ro
 inline size_t i8_split_offset(int64_t T, int64_t cols, int digits) {
     return (i8_scale_offset(T, cols, digits) + static_cast<size_t>(T) * 4 + 255) / 256 * 256;
 }
+// What a call needs is up to here; what a contraction's sharing needs on top, it needs only where a contraction is shared.  (The size never falls with T up to here,
+// but on the whole, where a longer batch shares nothing: a workspace for the longest batch has to serve shorter ones.)
+inline size_t i8_least_workspace_bytes(int64_t T, int64_t cols, int digits) { return i8_split_offset(T, cols, digits); }
 inline size_t i8_workspace_bytes(int64_t T, int64_t cols, int digits) {
     return i8_split_offset(T, cols, digits) + (i8_splits(T, cols, digits) ? kI8SplitTiles * (4 + 64 * 64 * 4) : 0);
 }

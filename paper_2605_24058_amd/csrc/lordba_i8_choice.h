@@ -60,9 +60,10 @@ inline Choice cheapest_tile(const TileCost (&tiles)[7], int64_t channels, int64_
     return best;
 }
 
-// The tile of T rows in `digits` digits with n outputs (of a gate and an up projection each) over `cols` columns
-inline Choice i8_choice(int64_t T, int64_t cols, int64_t n, int digits, bool gated) {
-    return cheapest_tile(gated ? kGatedTiles : kTiles, (gated ? 2 : 1) * n, digits * T, digits == 2, static_cast<int>(i8_pieces(cols)), i8_splits(T, cols, digits));
+// The tile of T rows in `digits` digits with n outputs (of a gate and an up projection each) over `cols` columns.  room: for a shared contraction's sums
+inline Choice i8_choice(int64_t T, int64_t cols, int64_t n, int digits, bool gated, bool room = true) {
+    return cheapest_tile(gated ? kGatedTiles : kTiles, (gated ? 2 : 1) * n, digits * T, digits == 2, static_cast<int>(i8_pieces(cols)),
+                         room && i8_splits(T, cols, digits));
 }
 
 constexpr size_t kLdsBytes = 160 * 1024;   // of a compute unit

@@ -540,7 +540,7 @@ lordba_status product_launch(const ProductArgs& a, hipStream_t stream) {
 
 template <int DIG, bool GATED>
 lordba_status product(ProductArgs a, hipStream_t stream) {
-    const Choice choice = i8_choice(a.T, 64 * static_cast<int64_t>(a.pieces), a.n, DIG, GATED);
+    const Choice choice = i8_choice(a.T, 64 * static_cast<int64_t>(a.pieces), a.n, DIG, GATED, a.arrived != nullptr);
     a.splits = choice.splits;
     switch (choice.tile) {
         case 0: return product_launch<256, 256, 4, 2, 1, 4, DIG, GATED>(a, stream);
@@ -588,18 +588,17 @@ bool aliased(const Span (&out)[NO], const Span (&in)[NI]) {
 struct Workspace {
     int8_t* q;
     float* scale;
-    uint32_t* arrived;
+    uint32_t* arrived;   // counters that the row kernel clears ahead of the product; null: the product's contraction is not shared
     int32_t* parts;
+    size_t bytes;        // that the call may write to
 };
-Workspace split(void* workspace, int64_t T, int64_t cols, int digits) {
+Workspace split(void* workspace, size_t bytes, int64_t T, int64_t cols, int digits) {
     char* const p = static_cast<char*>(workspace);
     char* const more = p + i8_split_offset(T, cols, digits);
-    return {reinterpret_cast<int8_t*>(p), reinterpret_cast<float*>(p + i8_scale_offset(T, cols, digits)), reinterpret_cast<uint32_t*>(more),
-            reinterpret_cast<int32_t*>(more + kI8SplitTiles * 4)};
+    const bool room = i8_splits(T, cols, digits) && bytes >= i8_workspace_bytes(T, cols, digits);
+    return {reinterpret_cast<int8_t*>(p), reinterpret_cast<float*>(p + i8_scale_offset(T, cols, digits)), room ? reinterpret_cast<uint32_t*>(more) : nullptr,
+            reinterpret_cast<int32_t*>(more + kI8SplitTiles * 4), room ? i8_workspace_bytes(T, cols, digits) : i8_least_workspace_bytes(T, cols, digits)};
 }
-
-// The counters that the row kernel clears ahead of the product, where there is room for them.
-uint32_t* split_arrivals(const Workspace& ws, int64_t T, int64_t cols, int digits) { return i8_splits(T, cols, digits) ? ws.arrived : nullptr; }
 
 // y = x diag(col_scale) W^T diag(w_scale) over `contracted` columns
 lordba_status linear(const void* x, const float* col_scale, const int8_t* w, const float* w_scale, void* y, void* workspace, size_t workspace_bytes,
@@ -607,20 +606,20 @@ lordba_status linear(const void* x, const float* col_scale, const int8_t* w, con
     if (T == 0) return LORDBA_OK;
     const float* scale = col_scale ? col_scale : w_scale;
     if (!x || !w || !scale || !y || !workspace) return LORDBA_ERR_NULL;
-    if (workspace_bytes < lordba_i8_workspace_bytes(T, contracted, digits)) return LORDBA_ERR_WORKSPACE;
+    if (workspace_bytes < i8_least_workspace_bytes(T, contracted, digits)) return LORDBA_ERR_WORKSPACE;
+    const Workspace ws = split(workspace, workspace_bytes, T, contracted, digits);
     if (i8_misaligned(x, 2) || i8_misaligned(w, 16) || i8_misaligned(scale, 4) || i8_misaligned(y, 2) || i8_misaligned(workspace, 16)) return LORDBA_ERR_ALIGN;
-    const Span out[] = {{y, static_cast<size_t>(T) * n * 2}, {workspace, lordba_i8_workspace_bytes(T, contracted, digits)}};
+    const Span out[] = {{y, static_cast<size_t>(T) * n * 2}, {workspace, ws.bytes}};
     const Span in[] = {{x, static_cast<size_t>(T) * contracted * 2}, {w, static_cast<size_t>(n) * i8_row_bytes(contracted)},
                        {scale, static_cast<size_t>(col_scale ? contracted : n) * 4}};
     if (aliased(out, in)) return LORDBA_ERR_ALIAS;
     const lordba_status dev = check_device();
     if (dev != LORDBA_OK) return dev;
     const hipStream_t st = static_cast<hipStream_t>(stream);
-    const Workspace ws = split(workspace, T, contracted, digits);
     const ProductArgs a = {w, ws.q, ws.scale, w_scale, nullptr, static_cast<_Float16*>(y), nullptr, T, n, i8_row_bytes(contracted), static_cast<int>(i8_pieces(contracted)),
                            static_cast<const _Float16*>(x), contracted, ws.parts, ws.arrived, 1, 0};
     if (const int own = col_scale ? 0 : i8_own_rows(T, contracted, digits, false, !i8_misaligned(x, 16))) return own_rows_product<false>(a, own, st);
-    const lordba_status rows = lordba_i8_quantize(x, col_scale, ws.q, ws.scale, split_arrivals(ws, T, contracted, digits), T, contracted, digits, st);
+    const lordba_status rows = lordba_i8_quantize(x, col_scale, ws.q, ws.scale, ws.arrived, T, contracted, digits, st);
     if (rows != LORDBA_OK) return rows;
     return digits == 1 ? product<1, false>(a, st) : product<2, false>(a, st);
 }
@@ -646,22 +645,22 @@ extern "C" lordba_status lordba_gated_i8(const void* x, const int8_t* W, const f
     lordba_status st = check(T, d_in, d_ff, d_in, digits);
     if (st != LORDBA_OK || T == 0) return st;
     if (!x || !W || !w_scale || !h || !workspace) return LORDBA_ERR_NULL;
-    if (workspace_bytes < lordba_i8_workspace_bytes(T, d_in, digits)) return LORDBA_ERR_WORKSPACE;
+    if (workspace_bytes < i8_least_workspace_bytes(T, d_in, digits)) return LORDBA_ERR_WORKSPACE;
+    const Workspace ws = split(workspace, workspace_bytes, T, d_in, digits);
     if (i8_misaligned(x, 2) || i8_misaligned(W, 16) || i8_misaligned(w_scale, 4) || i8_misaligned(addends, 2) || i8_misaligned(h, 2) ||
         i8_misaligned(gate_up, 2) || i8_misaligned(workspace, 16))
         return LORDBA_ERR_ALIGN;
     const size_t nh = static_cast<size_t>(T) * d_ff * 2;
-    const Span out[] = {{h, nh}, {gate_up, 2 * nh}, {workspace, lordba_i8_workspace_bytes(T, d_in, digits)}};
+    const Span out[] = {{h, nh}, {gate_up, 2 * nh}, {workspace, ws.bytes}};
     const Span in[] = {{x, static_cast<size_t>(T) * d_in * 2}, {W, static_cast<size_t>(2 * d_ff) * i8_row_bytes(d_in)},
                        {w_scale, static_cast<size_t>(2 * d_ff) * 4}, {addends, 2 * nh}};
     if (aliased(out, in)) return LORDBA_ERR_ALIAS;
     if ((st = check_device()) != LORDBA_OK) return st;
     const hipStream_t s = static_cast<hipStream_t>(stream);
-    const Workspace ws = split(workspace, T, d_in, digits);
     const ProductArgs a = {W, ws.q, ws.scale, w_scale, static_cast<const _Float16*>(addends), static_cast<_Float16*>(h), static_cast<_Float16*>(gate_up),
                            T, d_ff, i8_row_bytes(d_in), static_cast<int>(i8_pieces(d_in)), static_cast<const _Float16*>(x), d_in, ws.parts, ws.arrived, 1, 0};
     if (const int own = i8_own_rows(T, d_in, digits, true, !i8_misaligned(x, 16))) return own_rows_product<true>(a, own, s);
-    if ((st = lordba_i8_quantize(x, nullptr, ws.q, ws.scale, split_arrivals(ws, T, d_in, digits), T, d_in, digits, s)) != LORDBA_OK) return st;
+    if ((st = lordba_i8_quantize(x, nullptr, ws.q, ws.scale, ws.arrived, T, d_in, digits, s)) != LORDBA_OK) return st;
     return digits == 1 ? product<1, true>(a, s) : product<2, true>(a, s);
 }
 
@@ -671,18 +670,18 @@ extern "C" lordba_status lordba_gated_i8_backward(const void* dh, const void* ga
     lordba_status st = check(T, d_in, d_ff, 2 * d_ff, digits);
     if (st != LORDBA_OK || T == 0) return st;
     if (!dh || !gate_up || !Wt || !w_scale || !dx || !dgate_up || !workspace) return LORDBA_ERR_NULL;
-    if (workspace_bytes < lordba_i8_workspace_bytes(T, 2 * d_ff, digits)) return LORDBA_ERR_WORKSPACE;
+    if (workspace_bytes < i8_least_workspace_bytes(T, 2 * d_ff, digits)) return LORDBA_ERR_WORKSPACE;
+    const Workspace ws = split(workspace, workspace_bytes, T, 2 * d_ff, digits);
     if (i8_misaligned(dh, 2) || i8_misaligned(gate_up, 2) || i8_misaligned(Wt, 16) || i8_misaligned(w_scale, 4) || i8_misaligned(dx, 2) ||
         i8_misaligned(dgate_up, 2) || i8_misaligned(workspace, 16))
         return LORDBA_ERR_ALIGN;
     const size_t nh = static_cast<size_t>(T) * d_ff * 2;
-    const Span out[] = {{dx, static_cast<size_t>(T) * d_in * 2}, {dgate_up, 2 * nh}, {workspace, lordba_i8_workspace_bytes(T, 2 * d_ff, digits)}};
+    const Span out[] = {{dx, static_cast<size_t>(T) * d_in * 2}, {dgate_up, 2 * nh}, {workspace, ws.bytes}};
     const Span in[] = {{dh, nh}, {gate_up, 2 * nh}, {Wt, static_cast<size_t>(d_in) * i8_row_bytes(2 * d_ff)}, {w_scale, static_cast<size_t>(2 * d_ff) * 4}};
     if (aliased(out, in)) return LORDBA_ERR_ALIAS;
     if ((st = check_device()) != LORDBA_OK) return st;
     const hipStream_t s = static_cast<hipStream_t>(stream);
-    const Workspace ws = split(workspace, T, 2 * d_ff, digits);
-    if ((st = lordba_i8_gated_grad(dh, gate_up, w_scale, dgate_up, ws.q, ws.scale, split_arrivals(ws, T, 2 * d_ff, digits), T, d_ff, digits, s)) != LORDBA_OK) return st;
+    if ((st = lordba_i8_gated_grad(dh, gate_up, w_scale, dgate_up, ws.q, ws.scale, ws.arrived, T, d_ff, digits, s)) != LORDBA_OK) return st;
     const ProductArgs a = {Wt, ws.q, ws.scale, nullptr, nullptr, static_cast<_Float16*>(dx), nullptr, T, d_in, i8_row_bytes(2 * d_ff), static_cast<int>(i8_pieces(2 * d_ff)), nullptr, 0, ws.parts, ws.arrived, 1, 0};
     return digits == 1 ? product<1, false>(a, s) : product<2, false>(a, s);
 }
