@@ -459,7 +459,8 @@ lordba_status lordba_linear_i8_backward(const void* g, const int8_t* Wt, const f
  *   x fp16 [T, d_in]; W laid-out int8 [2 d_ff, .], the rows of Wg, then those of Wu; w_scale fp32 [2 d_ff];
  *   addends fp16 [2, T, d_ff] or NULL: what is added to the projections before the activation (the adapters' branches: lordba_forward with
  *   y_base = 0); h fp16 [T, d_ff]; gate_up fp16 [2, T, d_ff] or NULL: gate and up, kept for the backward pass.
- * gate and up enter h before they are rounded.  workspace: lordba_i8_workspace_bytes(T, d_in, digits).  Everything else as
+ * gate and up enter h before they are rounded.  In gate_up, what passes the range of fp16 is kept as its largest number of that sign (a NaN as a NaN): h may
+ * be a finite number where gate is none in fp16, and so are its gradients then.  workspace: lordba_i8_workspace_bytes(T, d_in, digits).  Everything else as
  * lordba_linear_i8; 1 <= d_ff <= 2^24. */
 lordba_status lordba_gated_i8(const void* x, const int8_t* W, const float* w_scale, const void* addends, void* h, void* gate_up,
                               void* workspace, size_t workspace_bytes, int64_t T, int64_t d_in, int64_t d_ff, int digits, void* stream);

@@ -51,15 +51,22 @@ __device__ __forceinline__ void load8(const float* p, int64_t c, int64_t n, floa
         for (int e = 0; e < 8; ++e) v[e] = p[min(c + e, n - 1)];
     }
 }
+// KEPT: for the backward pass.  What passes the range of fp16 is kept as its largest number (a NaN as one): with an infinity the slopes of the gated activation,
+// finite numbers here and h's too, would come out as 0 times infinity.
+template <bool KEPT>
 __device__ __forceinline__ u4 to_halves(const float (&f)[8]) {
     h8 h;
 #pragma unroll
     for (int e = 0; e < 8; ++e) h[e] = static_cast<_Float16>(f[e]);
+    if constexpr (KEPT) {
+        const h8 largest = static_cast<_Float16>(65504);
+        h = __builtin_elementwise_minimum(__builtin_elementwise_maximum(h, -largest), largest);
+    }
     return __builtin_bit_cast(u4, h);
 }
-template <bool FULL, bool STREAM = false>
+template <bool FULL, bool STREAM, bool KEPT>
 __device__ __forceinline__ void store8(_Float16* row, int64_t c, int64_t n, const float (&f)[8]) {
-    const u4 v = to_halves(f);
+    const u4 v = to_halves<KEPT>(f);
     if (FULL || c + 8 <= n) {
         if constexpr (STREAM) store16_any_stream(row + c, v);
         else *reinterpret_cast<u4_any*>(row + c) = v;
@@ -72,9 +79,10 @@ __device__ __forceinline__ void store8(_Float16* row, int64_t c, int64_t n, cons
 // The same for rows of which every other one starts in the middle of a word (an odd n), all lanes here: the four lane groups' 32 columns are stored
 // from their second column on, one further for each lane, so that the wide stores start on words (the memory path takes stores that do not apart).
 // 4096 x 8191 results 48 us -> 39 with 128 x 128 tiles, 50 -> 45 with 256 x 256.
+template <bool KEPT>
 __device__ __forceinline__ void store8_odd(_Float16* p, const float (&f)[8]) {
     typedef uint32_t u3_word __attribute__((ext_vector_type(3), aligned(4)));
-    const u4 v = to_halves(f);
+    const u4 v = to_halves<KEPT>(f);
     const int g = (threadIdx.x & 63) >> 4;
     const bool odd = (reinterpret_cast<uintptr_t>(p) & 2) != 0;
     const uint32_t next = static_cast<uint32_t>(__shfl_down(static_cast<int>(v[0]), 16));
@@ -142,17 +150,17 @@ __device__ __forceinline__ void finish(const ProductArgs& a, const i4 (&acc)[CB]
                 }
             if constexpr (GATED) {
                 if (a.kept && ODD) {
-                    store8_odd(a.kept + t * a.n + c, v[0]);
-                    store8_odd(a.kept + plane + t * a.n + c, v[1]);
+                    store8_odd<true>(a.kept + t * a.n + c, v[0]);
+                    store8_odd<true>(a.kept + plane + t * a.n + c, v[1]);
                 } else if (a.kept) {
-                    store8<FULL, LINES>(a.kept + t * a.n, c, a.n, v[0]);
-                    store8<FULL, LINES>(a.kept + plane + t * a.n, c, a.n, v[1]);
+                    store8<FULL, LINES, true>(a.kept + t * a.n, c, a.n, v[0]);
+                    store8<FULL, LINES, true>(a.kept + plane + t * a.n, c, a.n, v[1]);
                 }
 #pragma unroll
                 for (int e = 0; e < 8; ++e) v[0][e] = v[0][e] * __builtin_amdgcn_rcpf(1.f + __expf(-v[0][e])) * v[1][e];
             }
-            if constexpr (ODD) store8_odd(a.y + t * a.n + c, v[0]);
-            else store8<FULL, STREAM>(a.y + t * a.n, c, a.n, v[0]);
+            if constexpr (ODD) store8_odd<false>(a.y + t * a.n + c, v[0]);
+            else store8<FULL, STREAM, false>(a.y + t * a.n, c, a.n, v[0]);
         }
     }
 }
