@@ -409,10 +409,15 @@ lordba_status lordba_ptq_beta_solve(const double* G, const double* h, double* be
  *     amax_t = max_i |x[t, i]|,  D = 127 (digits = 1) or 127 * 256 (digits = 2)
  *     q[t, i] = rint(x[t, i] * (D / amax_t)),  s_t = amax_t / D         (fp32; ties to even; a row of zeros has s_t = 0)
  *     y[t, j] = fp16(s_t * w_scale[j] * sum_i q[t, i] * W[j, i])
- * digits = 1 holds a row in one int8 each, digits = 2 in two (q = 256 hi + lo, 16 bits): twice the multiplications, and a rounding of the
- * rows below that of fp16.  A row that holds an infinity or a NaN gives NaN in all of its results, in other rows nothing.
+ * digits = 1 holds a row in one int8 each, digits = 2 in two (q = 256 hi + lo, 16 bits): twice the multiplications.  The steps are those of the row's
+ * largest entry: every entry is off by up to half a step, amax / 254 or amax / 65024, and 2^-22 of itself (fp32).  With independent entries that is an
+ * error of the result of amax / rms times 2.3e-3 or 8.9e-6 of its norm.  The rounding of y to fp16 adds 2.1e-4: two digits stay below it while a
+ * row's largest entry is less than some 24 times its root mean square, and pass it in rows with larger outliers (amax / rms reaches the square root
+ * of the number of columns where one entry outweighs all others: 64 at 4096 columns, 5.7e-4).
+ * A row that holds an infinity or a NaN gives NaN in all of its results, in other rows nothing.
  * Laid-out matrices: int8 [rows, lordba_i8_row_bytes(cols)], row-major, zeros behind column cols.  lordba_layout_i8 brings plain int8
- * matrices into that form once; lordba_quantize_rows makes it from fp16 (weights, or rows of activations). */
+ * matrices into that form once; lordba_quantize_rows makes it from fp16 weights.  (The products take activations as fp16 and bring them to integers
+ * themselves; lordba_quantize_rows shows what they contract.) */
 #define LORDBA_I8_MAX_COLUMNS 131071   /* longest contraction whose sum stays inside 32 bits */
 
 /* Bytes from one row to the next of a laid-out int8 matrix (0 for cols outside 1 .. LORDBA_I8_MAX_COLUMNS). */
@@ -449,7 +454,7 @@ lordba_status lordba_linear_i8(const void* x, const int8_t* W, const float* w_sc
 
 /* DEVICE function: the gradient of y = x W^T with respect to x, dx[t, i] = sum_j g[t, j] w_scale[j] W[j, i] (what lordba_backward takes as
  * dx_base).  g fp16 [T, d_out]; Wt: the transposed layout of W, int8 [d_in, lordba_i8_row_bytes(d_out)]; w_scale fp32 [d_out]; dx fp16
- * [T, d_in].  The rows g * w_scale are held in `digits` digits: with 2 the error per entry of a row is at most its largest entry / 65024.
+ * [T, d_in].  The rows g * w_scale are held in `digits` digits, with the errors given above of rows (half a step of the row's largest |g * w_scale|).
  * workspace: lordba_i8_workspace_bytes(T, d_out, digits).  1 <= d_out <= LORDBA_I8_MAX_COLUMNS; everything else as lordba_linear_i8. */
 lordba_status lordba_linear_i8_backward(const void* g, const int8_t* Wt, const float* w_scale, void* dx, void* workspace, size_t workspace_bytes,
                                         int64_t T, int64_t d_in, int64_t d_out, int digits, void* stream);
@@ -470,7 +475,8 @@ lordba_status lordba_gated_i8(const void* x, const int8_t* W, const float* w_sca
  *     dx = dgate diag(w_scale) Wg + dup diag(w_scale) Wu
  *   Wt: the transposed layout of the [2 d_ff, d_in] weights, int8 [d_in, lordba_i8_row_bytes(2 d_ff)]; dx fp16 [T, d_in];
  *   dgate_up fp16 [2, T, d_ff]: dgate and dup, the upstream gradients of the two adapters (lordba_backward).
- * dx takes dgate and dup before they are rounded to fp16, one token's 2 d_ff numbers as one row of `digits` digits.
+ * dx takes dgate and dup before they are rounded to fp16, one token's 2 d_ff numbers times their scales as one row of `digits` digits, whose largest sets
+ * the step of both.
  * workspace: lordba_i8_workspace_bytes(T, 2 d_ff, digits).  2 d_ff <= LORDBA_I8_MAX_COLUMNS; everything else as lordba_linear_i8. */
 lordba_status lordba_gated_i8_backward(const void* dh, const void* gate_up, const int8_t* Wt, const float* w_scale, void* dx, void* dgate_up,
                                        void* workspace, size_t workspace_bytes, int64_t T, int64_t d_in, int64_t d_ff, int digits, void* stream);
@@ -483,7 +489,7 @@ lordba_status lordba_gated_i8_backward(const void* dh, const void* gate_up, cons
  * The backward pass is the same call on the gradient with the same seed and offset, with the base path's gradient as y_base.
  *   x, y_out fp16 [n]; y_base fp16 [n] or NULL (0); y_out may be x or y_base itself, any other overlap -> LORDBA_ERR_ALIAS.
  *   offset_dev: one uint64 in device memory or NULL (0): a program that replays a captured graph moves the mask by writing it.
- * p outside [0, 1] or NaN -> LORDBA_ERR_VALUE.  n <= 2^38.  Enqueues one kernel; never synchronises, allocates or frees. */
+ * p outside [0, 1] or NaN -> LORDBA_ERR_VALUE.  n <= 2^38.  Enqueues one kernel for every 2^34 elements; never synchronises, allocates or frees. */
 lordba_status lordba_dropout(const void* x, const void* y_base, void* y_out, int64_t n, double p, uint64_t seed, uint64_t offset,
                              const uint64_t* offset_dev, void* stream);
 

@@ -931,7 +931,7 @@ def lordba_quantize_rows(x, col_scale=None, digits: int = 1, stream=None):
 
 def lordba_linear_i8(x, W, w_scale, digits: int = 1, y_out=None, workspace=None, stream=None):
     """The frozen base projection y = x W^T on 8-bit weights: x fp16 [T, d_in], W the layout of int8 [d_out, d_in], w_scale fp32
-    [d_out]; the rows of x in one digit (8 bits) or two (16).  Returns y fp16 [T, d_out], what lordba_forward takes as y_base."""
+    [d_out]; the rows of x in one digit (8 bits) or two (16), in steps of their largest entry.  Returns y fp16 [T, d_out], what lordba_forward takes as y_base."""
     res = _plain_call("linear_i8", x, W, w_scale, digits, y_out, workspace, stream)
     if res is not None:
         return res
@@ -958,7 +958,8 @@ def lordba_linear_i8(x, W, w_scale, digits: int = 1, y_out=None, workspace=None,
 
 def lordba_linear_i8_backward(g, Wt, w_scale, digits: int = 2, dx_out=None, workspace=None, stream=None):
     """The gradient of that projection with respect to x: g fp16 [T, d_out], Wt the transposed layout of W, w_scale fp32 [d_out];
-    g * w_scale in two digits unless asked otherwise.  Returns dx fp16 [T, d_in], what lordba_backward takes as dx_base."""
+    g * w_scale in two digits unless asked otherwise: 16 bits in steps of a row's largest entry, which shows beside the rounding to fp16 in rows with an
+    entry 24 times their root mean square or more (include/lordba.h).  Returns dx fp16 [T, d_in], what lordba_backward takes as dx_base."""
     res = _plain_call("linear_i8_backward", g, Wt, w_scale, digits, dx_out, workspace, stream)
     if res is not None:
         return res
@@ -1019,6 +1020,7 @@ def lordba_gated_i8(x, W, w_scale, addends=None, digits: int = 1, save: bool = F
 
 def lordba_gated_i8_backward(dh, gate_up, Wt, w_scale, digits: int = 2, workspace=None, stream=None):
     """Backward pass of lordba_gated_i8: dh fp16 [T, d_ff], the kept gate_up, Wt the transposed layout of the [2 d_ff, d_in] weights.
+    dx contracts a token's dgate and dup in two digits unless asked otherwise (as lordba_linear_i8_backward).
     Returns (dx fp16 [T, d_in], dgate_up fp16 [2, T, d_ff]); dgate_up holds the upstream gradients of the two adapters."""
     res = _plain_call("gated_i8_backward", dh, gate_up, Wt, w_scale, digits, workspace, stream)
     if res is not None:
