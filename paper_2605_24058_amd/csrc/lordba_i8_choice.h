@@ -21,8 +21,10 @@ inline bool i8_splits(int64_t T, int64_t cols, int digits) { return i8_row_bytes
 
 // The tiles and their times on a compute unit, in nanoseconds: a step of 64 columns alone on a chip with few workgroups (waiting; 1.4 times that where the
 // weights are read once or come from memory), the same as a share of a chip that is full (throughput; small tiles run side by side on a unit), and what comes around
-// the steps, filling and results.  Fitted to some forty shapes of 1 to 16384 rows, 64 to 13824 columns, even and odd; the tile with the least sum was the
-// fastest of the six or within 15 % of it on all but a few of them (6536 x 129 x 1910 gated: 26 us instead of 19).
+// the steps, filling and results.  Fitted to some forty shapes.  On 200 others (5 to 16384 rows, 64 to 13824 columns, one and two digits, gated or not, half of
+// them with weights that no cache holds), every tile timed with a shared contraction and without: the way with the least sum was the fastest on 140, within 5 % of it
+// on 160, within 15 % on 187, and 35 % behind at worst (389 x 67 x 5734 gated 14.7 us instead of 10.9 with 128 x 128 tiles, 3575 x 7716 -> 348 54 instead
+// of 41 with 64 x 64); 2.8 % behind in the mean.
 struct TileCost {
     int channels, tokens;
     double alone, share, fixed;

@@ -13,7 +13,7 @@ def test_what_near_refuses():
     good = one.astype(np.float16)
     near(good, one, none)
     past = np.full((2, 3), -1e5)
-    near(past.astype(np.float16), past, none)
+    near(np.full((2, 3), -np.inf, np.float16), past, none)
     near(np.full((2, 3), -65504, np.float16), np.full((2, 3), -65510.0), none)
     bad = good.copy()
     for v in (np.nan, np.inf, -np.inf, 1.002, 0):
@@ -24,7 +24,7 @@ def test_what_near_refuses():
         with pytest.raises(AssertionError):
             near(good, want, err)
     with pytest.raises(AssertionError):
-        near(-past.astype(np.float16), past, none)
+        near(np.full((2, 3), np.inf, np.float16), past, none)
     with pytest.raises(AssertionError):
         near(np.full((2, 3), -65504, np.float16), past, none)
 
