@@ -41,7 +41,7 @@ enum {
     LORDBA_ERR_DIM = 2,       /* T < 0, d_in < 1, d_out < 1, r < 1, r > LORDBA_MAX_RANK, or a
                                  size that does not fit 32-bit indexing of one row             */
     LORDBA_ERR_VALUE = 3,     /* a sign entry that is not +-1 (int8 variant) or is NaN (f32); a parameter
-                                 outside its range (tau, mu, digits, p)                          */
+                                 outside its range (tau, mu, digits, p, group, halves, temperature, type) */
     LORDBA_ERR_ALIAS = 4,     /* y_out overlaps an input other than being exactly y_base      */
     LORDBA_ERR_ALIGN = 5,     /* a pointer is not aligned to its element size                 */
     LORDBA_ERR_NO_DEVICE = 6, /* no usable HIP device / not a gfx950 device                   */
@@ -492,6 +492,95 @@ lordba_status lordba_gated_i8_backward(const void* dh, const void* gate_up, cons
  * p outside [0, 1] or NaN -> LORDBA_ERR_VALUE.  n <= 2^38.  Enqueues one kernel for every 2^34 elements; never synchronises, allocates or frees. */
 lordba_status lordba_dropout(const void* x, const void* y_base, void* y_out, int64_t n, double p, uint64_t seed, uint64_t offset,
                              const uint64_t* offset_dev, void* stream);
+
+/* ---- the frozen base on 4-bit weights, and learning from a teacher -------------------------------------------------- */
+
+/* The base projections on 4-bit weights with group scales,
+ *     W[j, i] = scale[j, i / group] * (code[j, i] - zero[j, i / group]),   group = 32, 64 or 128 columns of a row,
+ * codes and zeros whole numbers from 0 to 15 (their low four bits count; zeros that are not given are 8), scales finite fp16 numbers.  Activations, results and
+ * gradients are fp16.  Sums are held in fp32 and rounded once.
+ *     up to LORDBA_I4_FEW tokens, forward: a group's sum of x * (code - zero), each factor exact, is multiplied by its scale in fp32
+ *     more tokens, and every gradient: scale * (code - zero) is rounded to fp16 first, half a step (2^-11 of the weight) at most: relative to the norms of
+ *     what is summed 1.7e-4 in the root mean square, beside 2.1e-4 from the rounding of the result.  So |15 scale| has to be in the range of fp16.
+ * lordba_quantize_i4 makes codes and scales from fp16 weights, lordba_layout_i4 brings them once into the form that the products read, as W or as its
+ * transpose (for the gradients).  The matrices of the gated block have two halves, gate's rows and then up's. */
+#define LORDBA_I4_FEW 64
+
+/* Bytes of the laid-out codes of a matrix W [rows, cols], and the number of fp16 scales (and of zeros) that go with them; 0 for arguments out of range.
+ * rows, cols <= 2^24; halves: 1, or 2 with an even number of rows; transposed: the layout of W's transpose. */
+size_t lordba_i4_code_bytes(int64_t rows, int64_t cols, int halves, int transposed);
+size_t lordba_i4_scale_count(int64_t rows, int64_t cols, int64_t group, int halves, int transposed);
+
+/* DEVICE function: fp16 weights w [rows, cols] (contiguous) to codes, a byte each [rows, cols], scales fp16 [rows, ceil(cols / group)] and zeros, a byte
+ * each [rows, ceil(cols / group)], or NULL for symmetric codes:
+ *     symmetric: scale = fp16(amax / 7), zero = 8;   with zeros: scale = fp16((high - low) / 15), zero = rint(-low / scale) to 15 at most, where low <= 0 <= high
+ *     code = rint(w / scale + zero) between 0 and 15                                                          (fp32; ties to even)
+ * A group whose scale is 0 gets codes that stand for 0; one that holds an infinity or a NaN the scale NaN.  group other than 32, 64, 128 -> LORDBA_ERR_VALUE. */
+lordba_status lordba_quantize_i4(const void* w, uint8_t* codes, void* scale, uint8_t* zero, int64_t rows, int64_t cols, int64_t group, void* stream);
+
+/* DEVICE function: lays out codes, scales and zeros (or NULL) as above.  out: lordba_i4_code_bytes bytes; out_scale, out_zero (unread if zero is NULL):
+ * lordba_i4_scale_count fp16 numbers each; all three 16-byte aligned, no overlap with the inputs or each other. */
+lordba_status lordba_layout_i4(const uint8_t* codes, const void* scale, const uint8_t* zero, uint8_t* out, void* out_scale, void* out_zero, int64_t rows,
+                               int64_t cols, int64_t group, int halves, int transposed, void* stream);
+
+/* DEVICE function: y = x W^T.  x fp16 [T, d_in]; codes, scale, zero (or NULL): the layout of W [d_out, d_in]; y fp16 [T, d_out].  Any T >= 0 (0: no work),
+ * 1 <= d_in, d_out <= 2^24; activations aligned to their elements.  Needs no workspace; only enqueues kernels on `stream`, never
+ * synchronises, allocates or frees.  No output may overlap an input or another output (LORDBA_ERR_ALIAS). */
+lordba_status lordba_linear_i4(const void* x, const uint8_t* codes, const void* scale, const void* zero, void* y, int64_t T, int64_t d_in, int64_t d_out,
+                               int64_t group, void* stream);
+
+/* DEVICE function: its gradient with respect to x, dx = g W.  g fp16 [T, d_out]; codes_t, scale_t, zero_t (or NULL): the transposed layout of
+ * W [d_out, d_in]; dx fp16 [T, d_in].  Everything else as lordba_linear_i4. */
+lordba_status lordba_linear_i4_backward(const void* g, const uint8_t* codes_t, const void* scale_t, const void* zero_t, void* dx, int64_t T, int64_t d_in,
+                                        int64_t d_out, int64_t group, void* stream);
+
+/* DEVICE function: the gated feed-forward block's first half, as lordba_gated_i8, on the layout of W [2 d_ff, d_in] in two halves.
+ *   addends fp16 [2, T, d_ff] or NULL; h fp16 [T, d_ff]; gate_up fp16 [2, T, d_ff] or NULL: gate and up, kept for the backward pass.
+ * gate and up enter h before they are rounded; what passes the range of fp16 is kept as its largest number of that sign.  2 d_ff <= 2^24.  Everything
+ * else as lordba_linear_i4. */
+lordba_status lordba_gated_i4(const void* x, const uint8_t* codes, const void* scale, const void* zero, const void* addends, void* h, void* gate_up,
+                              int64_t T, int64_t d_in, int64_t d_ff, int64_t group, void* stream);
+
+/* DEVICE function: its backward pass, from dh fp16 [T, d_ff] and the kept gate_up:
+ *     dgate = dh * up * sigma(gate) * (1 + gate * (1 - sigma(gate))),  dup = dh * gate * sigma(gate),  dx = dgate Wg + dup Wu
+ * with the transposed layout of W [2 d_ff, d_in] in two halves; dx fp16 [T, d_in]; dgate_up fp16 [2, T, d_ff]: dgate and dup, of which, rounded, dx is
+ * made.  Everything else as lordba_linear_i4. */
+lordba_status lordba_gated_i4_backward(const void* dh, const void* gate_up, const uint8_t* codes_t, const void* scale_t, const void* zero_t, void* dx,
+                                       void* dgate_up, int64_t T, int64_t d_in, int64_t d_ff, int64_t group, void* stream);
+
+/* Learning from a teacher's top logits.  For a token with the student's logits z [V], the teacher's logits l_i at the vocabulary entries v_i (i < k), a
+ * label c and the temperature u:
+ *     p = softmax over the entries that are there of l_i / u,   q = softmax(z / u),   r = softmax(z)
+ *     loss = soft * u^2 * sum_i p_i (log p_i - log q[v_i]) - hard * log r[c]
+ *     d_logits = d_loss * (soft * u * (q - sum_i p_i onehot(v_i)) + hard * (r - onehot(c)))
+ * An entry is there if 0 <= v_i < V and l_i is not -infinity; the first term is 0 for a token with none.  A label outside [0, V) is none, and the second
+ * term is 0 then.  With neither, and with a term's factor 0, the term is not evaluated: loss and gradient are 0 whatever the logits hold.  An index that stands twice
+ * counts twice.  Logits of -infinity have probability 0.  A token whose evaluated logits hold a NaN or +infinity, or nothing but -infinity, gives NaN in
+ * its own loss and gradient; a NaN or +infinity among its teacher's entries that are there, in its loss and its gradient at those entries. */
+enum { LORDBA_F16 = 0, LORDBA_F32 = 1 };
+typedef struct {
+    const int32_t* top_index;  /* [T, k], or NULL with k = 0                                   */
+    const void* top_logits;    /* [T, k], of the logits' type                                  */
+    const int32_t* labels;     /* [T], or NULL: none                                           */
+    int64_t k;                 /* 0 .. LORDBA_MAX_TOP                                          */
+    float temperature;         /* > 0                                                          */
+    float soft, hard;          /* factors of the two terms, finite                             */
+} lordba_teacher;
+#define LORDBA_MAX_TOP 1024
+
+/* DEVICE function: the tokens' losses, and with d_loss their gradients in the same pass.
+ *   logits [T, V] of `type` (LORDBA_F16, LORDBA_F32); loss fp32 [T]
+ *   d_loss fp32 [T] or NULL; d_logits [T, V] of `type`, given exactly if d_loss is; it may be the logits themselves
+ *   kept fp32 [T, 3] or NULL, for lordba_distill_backward: the largest logit m, sum exp((z - m) / u) and sum exp(z - m) (the first of the sums in the
+ *   place of both where one serves; zeros for a token with neither term)
+ * T >= 0, 1 <= V <= 2^24.  One workgroup a token; sums are fp32 in a fixed order.  Enqueues kernels only; never synchronises, allocates or frees.
+ * Tensors aligned to their elements; no other overlap of outputs with anything (LORDBA_ERR_ALIAS). */
+lordba_status lordba_distill(const void* logits, int type, const lordba_teacher* teacher, const float* d_loss, float* loss, float* kept, void* d_logits,
+                             int64_t T, int64_t V, void* stream);
+
+/* DEVICE function: the gradient behind the loss, from the logits and what the loss kept.  d_logits may be the logits themselves. */
+lordba_status lordba_distill_backward(const float* d_loss, const void* logits, int type, const float* kept, const lordba_teacher* teacher, void* d_logits,
+                                      int64_t T, int64_t V, void* stream);
 
 /* Static, never-NULL description of a status code. */
 const char* lordba_status_string(lordba_status status);

@@ -15,7 +15,7 @@ import subprocess
 import sys
 import sysconfig
 import warnings
-from typing import Optional, Tuple
+from typing import Any, NamedTuple, Optional, Tuple
 
 import numpy as np
 
@@ -27,7 +27,9 @@ _LIB_PATH = os.path.join(_PKG, "liblordba.so")
 _SOURCES = ("lordba_forward.hip", "lordba_forward_train.hip", "lordba_forward_any.hip", "lordba_forward_any_train.hip",
             "lordba_forward_multi_l2.hip", "lordba_forward_multi_l3.hip", "lordba_forward_multi_l4.hip",
             "lordba_forward_multi_train.hip", "lordba_forward_multi.hip", "lordba_backward.hip", "lordba_ptq.hip", "lordba_pack_device.hip", "lordba_pack.cpp",
-            "lordba_i8_rows.hip", "lordba_i8_product.hip", "lordba_dropout.hip")
+            "lordba_i8_rows.hip", "lordba_i8_product.hip", "lordba_dropout.hip",
+            "lordba_i4_rows.hip", "lordba_i4_few.hip", "lordba_i4_many.hip", "lordba_i4_calls.hip",
+            "lordba_distill.hip")
 _lib = None
 _TORCH_MODULE_PATH = os.path.join(_PKG, "_lordba_torch.so")
 _torch_module = None
@@ -43,6 +45,12 @@ class LordbaError(RuntimeError):
     def __init__(self, status: int, where: str):
         self.status = status
         super().__init__("%s failed: status %d (%s)" % (where, status, lordba_status_string(status)))
+
+
+class Teacher(ctypes.Structure):
+    """lordba_teacher of include/lordba.h"""
+    _fields_ = [("top_index", ctypes.c_void_p), ("top_logits", ctypes.c_void_p), ("labels", ctypes.c_void_p), ("k", ctypes.c_int64),
+                ("temperature", ctypes.c_float), ("soft", ctypes.c_float), ("hard", ctypes.c_float)]
 
 
 def build_library(verbose: bool = False) -> str:
@@ -238,6 +246,22 @@ def load_library():
         f.argtypes = [vp] * 7 + [ctypes.c_size_t] + [i64] * 3 + [ci, vp]
     lib.lordba_dropout.restype = ci
     lib.lordba_dropout.argtypes = [vp] * 3 + [i64, ctypes.c_double, ctypes.c_uint64, ctypes.c_uint64, vp, vp]
+    lib.lordba_i4_code_bytes.restype = ctypes.c_size_t
+    lib.lordba_i4_code_bytes.argtypes = [i64, i64, ci, ci]
+    lib.lordba_i4_scale_count.restype = ctypes.c_size_t
+    lib.lordba_i4_scale_count.argtypes = [i64, i64, i64, ci, ci]
+    lib.lordba_quantize_i4.restype = ci
+    lib.lordba_quantize_i4.argtypes = [vp] * 4 + [i64] * 3 + [vp]
+    lib.lordba_layout_i4.restype = ci
+    lib.lordba_layout_i4.argtypes = [vp] * 6 + [i64] * 3 + [ci, ci, vp]
+    for name, pointers in (("lordba_linear_i4", 5), ("lordba_linear_i4_backward", 5), ("lordba_gated_i4", 7), ("lordba_gated_i4_backward", 7)):
+        f = getattr(lib, name)
+        f.restype = ci
+        f.argtypes = [vp] * pointers + [i64] * 4 + [vp]
+    lib.lordba_distill.restype = ci
+    lib.lordba_distill.argtypes = [vp, ci, ctypes.POINTER(Teacher)] + [vp] * 4 + [i64, i64, vp]
+    lib.lordba_distill_backward.restype = ci
+    lib.lordba_distill_backward.argtypes = [vp, vp, ci, vp, ctypes.POINTER(Teacher), vp, i64, i64, vp]
     lib.lordba_status_string.restype = ctypes.c_char_p
     lib.lordba_status_string.argtypes = [ci]
     _lib = lib
@@ -1075,3 +1099,280 @@ def lordba_dropout(x, p: float, seed: int, offset: int = 0, y_base=None, y_out=N
     if st != 0:
         raise LordbaError(st, "lordba_dropout")
     return y_out
+
+
+class WeightsI4(NamedTuple):
+    """A matrix on 4-bit weights as the projections take it: what lordba_layout_i4 makes of W [rows, cols]."""
+    codes: Any          # uint8, laid out
+    scale: Any          # float16, in the codes' order
+    zero: Any           # the same, or None: 8 everywhere
+    rows: int
+    cols: int
+    group: int
+    halves: int
+    transposed: bool
+
+
+def lordba_quantize_i4(w, group: int = 128, zero_points: bool = False, stream=None):
+    """fp16 weights w [rows, cols] on 4 bits: (codes uint8 [rows, cols], scale fp16 [rows, groups], zero uint8 [rows, groups] or None) with
+    w ~ scale * (code - zero) for every `group` columns of a row, zero 8 where None; zero_points: the range of a group from its smallest to its largest."""
+    import torch
+
+    lib = load_library()
+    _need(torch.float16, "float16 CUDA tensor", ("w",), w)
+    if w.dim() != 2:
+        raise ValueError("w must be [rows, cols]")
+    if group not in (32, 64, 128):
+        raise ValueError("group must be 32, 64 or 128")
+    rows, cols = w.shape
+    with _on_stream(stream):
+        codes = torch.empty((rows, cols), dtype=torch.uint8, device=w.device)
+        scale = torch.empty((rows, -(-cols // group)), dtype=torch.float16, device=w.device)
+        zero = torch.empty(scale.shape, dtype=torch.uint8, device=w.device) if zero_points else None
+    st = lib.lordba_quantize_i4(w.data_ptr(), codes.data_ptr(), scale.data_ptr(), None if zero is None else zero.data_ptr(), rows, cols, group,
+                                _stream_handle(w, stream))
+    if st != 0:
+        raise LordbaError(st, "lordba_quantize_i4")
+    return codes, scale, zero
+
+
+def lordba_layout_i4(codes, scale, zero=None, group: int = 128, halves: int = 1, transposed: bool = False, stream=None) -> WeightsI4:
+    """Lays out 4-bit weights for the projections, once: codes uint8 [rows, cols], scale fp16 [rows, groups], zero uint8 [rows, groups] or None (8);
+    halves=2: the rows of a gate projection, then as many of an up projection; transposed: what the input gradients take."""
+    import torch
+
+    lib = load_library()
+    _need(torch.uint8, "uint8 CUDA tensor", ("codes",), codes)
+    _need(torch.float16, "float16 CUDA tensor", ("scale",), scale)
+    if codes.dim() != 2 or codes.numel() == 0:
+        raise ValueError("codes must be [rows, cols]")
+    if group not in (32, 64, 128):
+        raise ValueError("group must be 32, 64 or 128")
+    rows, cols = codes.shape
+    if halves not in (1, 2) or rows % halves:
+        raise ValueError("halves must be 1, or 2 with an even number of rows")
+    if tuple(scale.shape) != (rows, -(-cols // group)):
+        raise ValueError("scale must be [rows, groups]")
+    if zero is not None:
+        _need(torch.uint8, "uint8 CUDA tensor", ("zero",), zero)
+        if zero.shape != scale.shape:
+            raise ValueError("zero must be [rows, groups]")
+    n = lib.lordba_i4_scale_count(rows, cols, group, halves, int(bool(transposed)))
+    with _on_stream(stream):
+        out = torch.empty(lib.lordba_i4_code_bytes(rows, cols, halves, int(bool(transposed))), dtype=torch.uint8, device=codes.device)
+        out_scale = torch.empty(n, dtype=torch.float16, device=codes.device)
+        out_zero = None if zero is None else torch.empty_like(out_scale)
+    ptr = lambda t_: None if t_ is None else t_.data_ptr()
+    st = lib.lordba_layout_i4(codes.data_ptr(), scale.data_ptr(), ptr(zero), out.data_ptr(), out_scale.data_ptr(), ptr(out_zero), rows, cols, group, halves,
+                              int(bool(transposed)), _stream_handle(codes, stream))
+    if st != 0:
+        raise LordbaError(st, "lordba_layout_i4")
+    return WeightsI4(out, out_scale, out_zero, rows, cols, group, halves, bool(transposed))
+
+
+def _weights_i4(W, halves: int, transposed: bool, what: str) -> None:
+    import torch
+
+    if not isinstance(W, WeightsI4):
+        raise TypeError("%s must be what lordba_layout_i4 returns" % what)
+    if W.halves != halves or bool(W.transposed) is not transposed:
+        raise ValueError("%s must be laid out with halves=%d, transposed=%s" % (what, halves, transposed))
+    lib = load_library()
+    _need(torch.uint8, "uint8 CUDA tensor", (what + ".codes",), W.codes)
+    for name, t_ in (("scale", W.scale), ("zero", W.zero)):
+        if t_ is not None:
+            _need(torch.float16, "float16 CUDA tensor", ("%s.%s" % (what, name),), t_)
+    n = lib.lordba_i4_scale_count(W.rows, W.cols, W.group, halves, int(transposed))
+    if n == 0 or W.codes.numel() != lib.lordba_i4_code_bytes(W.rows, W.cols, halves, int(transposed)) or W.scale.numel() != n or \
+            (W.zero is not None and W.zero.numel() != n):
+        raise ValueError("%s is not the layout of its sizes" % what)
+
+
+def _linear_i4(name: str, x, W, y_out, stream, backward: bool):
+    import torch
+
+    lib = load_library()
+    _need(torch.float16, "float16 CUDA tensor", ("g" if backward else "x",), x)
+    _weights_i4(W, 1, backward, "Wt" if backward else "W")
+    k, n = (W.rows, W.cols) if backward else (W.cols, W.rows)
+    if x.dim() != 2 or x.shape[1] != k:
+        raise ValueError("%s must be [T, %d]" % ("g" if backward else "x", k))
+    T = x.shape[0]
+    with _on_stream(stream):
+        y_out = _output(y_out, (T, n), x, "dx_out" if backward else "y_out")
+    st = getattr(lib, name)(x.data_ptr(), W.codes.data_ptr(), W.scale.data_ptr(), None if W.zero is None else W.zero.data_ptr(), y_out.data_ptr(), T,
+                            W.cols, W.rows, W.group, _stream_handle(x, stream))
+    if st != 0:
+        raise LordbaError(st, name)
+    return y_out
+
+
+def lordba_linear_i4(x, W: WeightsI4, y_out=None, stream=None):
+    """The frozen base projection y = x W^T on 4-bit weights: x fp16 [T, d_in], W from lordba_layout_i4.  Returns y fp16 [T, d_out], what
+    lordba_forward takes as y_base."""
+    res = _plain_call("linear_i4", x, W, y_out, stream)
+    return _linear_i4("lordba_linear_i4", x, W, y_out, stream, False) if res is None else res
+
+
+def lordba_linear_i4_backward(g, Wt: WeightsI4, dx_out=None, stream=None):
+    """The gradient of that projection with respect to x: g fp16 [T, d_out], Wt the transposed layout of W.  Returns dx fp16 [T, d_in], what
+    lordba_backward takes as dx_base."""
+    res = _plain_call("linear_i4_backward", g, Wt, dx_out, stream)
+    return _linear_i4("lordba_linear_i4_backward", g, Wt, dx_out, stream, True) if res is None else res
+
+
+def lordba_gated_i4(x, W: WeightsI4, addends=None, save: bool = False, stream=None):
+    """h = silu(x Wg^T + addends[0]) * (x Wu^T + addends[1]) on 4-bit weights: x fp16 [T, d_in]; W the layout of [2 d_ff, d_in] with halves=2; addends
+    fp16 [2, T, d_ff]: the branches of the two projections' adapters.
+    Returns h fp16 [T, d_ff]; save: (h, gate_up) with gate_up fp16 [2, T, d_ff] for lordba_gated_i4_backward."""
+    res = _plain_call("gated_i4", x, W, addends, save, stream)
+    if res is not None:
+        return res
+    import torch
+
+    lib = load_library()
+    _need(torch.float16, "float16 CUDA tensor", ("x",), x)
+    _weights_i4(W, 2, False, "W")
+    if x.dim() != 2 or x.shape[1] != W.cols:
+        raise ValueError("x must be [T, %d]" % W.cols)
+    T, d_in = x.shape
+    d_ff = W.rows // 2
+    if addends is not None:
+        _need(torch.float16, "float16 CUDA tensor", ("addends",), addends)
+        if tuple(addends.shape) != (2, T, d_ff):
+            raise ValueError("addends must be [2, T, d_ff]")
+    with _on_stream(stream):
+        h = _output(None, (T, d_ff), x, "h")
+        gate_up = _output(None, (2, T, d_ff), x, "gate_up") if save else None
+    ptr = lambda t_: None if t_ is None else t_.data_ptr()
+    st = lib.lordba_gated_i4(x.data_ptr(), W.codes.data_ptr(), W.scale.data_ptr(), ptr(W.zero), ptr(addends), h.data_ptr(), ptr(gate_up), T, d_in, d_ff,
+                             W.group, _stream_handle(x, stream))
+    if st != 0:
+        raise LordbaError(st, "lordba_gated_i4")
+    return (h, gate_up) if save else h
+
+
+def lordba_gated_i4_backward(dh, gate_up, Wt: WeightsI4, stream=None):
+    """Backward pass of lordba_gated_i4: dh fp16 [T, d_ff], the kept gate_up, Wt the transposed layout of the [2 d_ff, d_in] weights with halves=2.
+    Returns (dx fp16 [T, d_in], dgate_up fp16 [2, T, d_ff]); dgate_up holds the upstream gradients of the two adapters."""
+    res = _plain_call("gated_i4_backward", dh, gate_up, Wt, stream)
+    if res is not None:
+        return res
+    import torch
+
+    lib = load_library()
+    _need(torch.float16, "float16 CUDA tensor", ("dh", "gate_up"), dh, gate_up)
+    _weights_i4(Wt, 2, True, "Wt")
+    if dh.dim() != 2 or 2 * dh.shape[1] != Wt.rows or tuple(gate_up.shape) != (2,) + tuple(dh.shape):
+        raise ValueError("dh must be [T, %d], gate_up [2, T, %d]" % (Wt.rows // 2, Wt.rows // 2))
+    T, d_ff = dh.shape
+    d_in = Wt.cols
+    with _on_stream(stream):
+        dx, dgate_up = _output(None, (T, d_in), dh, "dx"), _output(None, (2, T, d_ff), dh, "dgate_up")
+    st = lib.lordba_gated_i4_backward(dh.data_ptr(), gate_up.data_ptr(), Wt.codes.data_ptr(), Wt.scale.data_ptr(),
+                                      None if Wt.zero is None else Wt.zero.data_ptr(), dx.data_ptr(), dgate_up.data_ptr(), T, d_in, d_ff, Wt.group,
+                                      _stream_handle(dh, stream))
+    if st != 0:
+        raise LordbaError(st, "lordba_gated_i4_backward")
+    return dx, dgate_up
+
+
+def _teacher(logits, top_index, top_logits, labels, temperature, soft, hard) -> Teacher:
+    import torch
+
+    if logits.dtype not in (torch.float16, torch.float32):
+        raise TypeError("logits must be a contiguous float16 or float32 CUDA tensor")
+    kind = "%s CUDA tensor" % str(logits.dtype).split(".")[1]
+    _need(logits.dtype, kind, ("logits",), logits)
+    if logits.dim() != 2 or logits.shape[1] < 1:
+        raise ValueError("logits must be [T, V]")
+    if (top_index is None) != (top_logits is None):
+        raise ValueError("top_index and top_logits come together")
+    k = 0
+    if top_index is not None:
+        _need(torch.int32, "int32 CUDA tensor", ("top_index",), top_index)
+        _need(logits.dtype, kind, ("top_logits",), top_logits)
+        if top_index.dim() != 2 or top_index.shape[0] != logits.shape[0] or top_logits.shape != top_index.shape:
+            raise ValueError("top_index and top_logits must be [T, k]")
+        k = top_index.shape[1]
+    if labels is not None:
+        _need(torch.int32, "int32 CUDA tensor", ("labels",), labels)
+        if tuple(labels.shape) != (logits.shape[0],):
+            raise ValueError("labels must be [T]")
+    ptr = lambda t_: None if t_ is None or t_.numel() == 0 else t_.data_ptr()
+    return Teacher(ptr(top_index), ptr(top_logits), ptr(labels), k, temperature, soft, hard)
+
+
+def _per_token(given, T, what: str):
+    import torch
+
+    _need(torch.float32, "float32 CUDA tensor", (what,), given)
+    if tuple(given.shape) != (T,):
+        raise ValueError("%s must be [T]" % what)
+
+
+def _logits_out(given, logits):
+    import torch
+
+    if given is None:
+        return torch.empty_like(logits)
+    _need(logits.dtype, "%s CUDA tensor" % str(logits.dtype).split(".")[1], ("d_logits_out",), given)
+    if given.shape != logits.shape:
+        raise ValueError("d_logits_out must have the shape of logits")
+    return given
+
+
+def lordba_distill(logits, top_index=None, top_logits=None, labels=None, temperature: float = 1.0, soft: float = 1.0, hard: float = 0.0, d_loss=None,
+                   d_logits_out=None, stream=None):
+    """What tokens lose against a teacher's top logits: logits [T, V] fp16 or fp32; top_index int32 [T, k] (an index outside [0, V): no entry), top_logits
+    [T, k] of the logits' type; labels int32 [T] or None (outside [0, V): none).  soft * temperature^2 * KL(teacher || student) over the entries that
+    are there, at the temperature, plus hard * the label's cross entropy; a token with neither loses 0.
+    Returns (loss fp32 [T], kept fp32 [T, 3] for lordba_distill_backward); with d_loss fp32 [T], the tokens' weights, (loss, d_logits) in one pass.
+    d_logits_out may be the logits themselves."""
+    res = _plain_call("distill", logits, top_index, top_logits, labels, temperature, soft, hard, d_loss, d_logits_out, stream)
+    if res is not None:
+        return res
+    import torch
+
+    lib = load_library()
+    teacher = _teacher(logits, top_index, top_logits, labels, temperature, soft, hard)
+    T, V = logits.shape
+    if d_loss is None and d_logits_out is not None:
+        raise ValueError("d_logits_out needs d_loss")
+    if d_loss is not None:
+        _per_token(d_loss, T, "d_loss")
+    with _on_stream(stream):
+        loss = torch.empty(T, dtype=torch.float32, device=logits.device)
+        kept = torch.empty((T, 3), dtype=torch.float32, device=logits.device) if d_loss is None else None
+        d_logits = None if d_loss is None else _logits_out(d_logits_out, logits)
+    ptr = lambda t_: None if t_ is None else t_.data_ptr()
+    st = lib.lordba_distill(logits.data_ptr(), int(logits.dtype is torch.float32), ctypes.byref(teacher), ptr(d_loss), loss.data_ptr(), ptr(kept), ptr(d_logits),
+                            T, V, _stream_handle(logits, stream))
+    if st != 0:
+        raise LordbaError(st, "lordba_distill")
+    return loss, kept if d_loss is None else d_logits
+
+
+def lordba_distill_backward(d_loss, logits, kept, top_index=None, top_logits=None, labels=None, temperature: float = 1.0, soft: float = 1.0,
+                            hard: float = 0.0, d_logits_out=None, stream=None):
+    """The gradient of lordba_distill's losses with respect to the logits, each token's times d_loss fp32 [T]; kept and the other arguments as there.
+    Returns d_logits of the logits' type; d_logits_out may be the logits themselves."""
+    res = _plain_call("distill_backward", d_loss, logits, kept, top_index, top_logits, labels, temperature, soft, hard, d_logits_out, stream)
+    if res is not None:
+        return res
+    import torch
+
+    lib = load_library()
+    teacher = _teacher(logits, top_index, top_logits, labels, temperature, soft, hard)
+    T, V = logits.shape
+    _per_token(d_loss, T, "d_loss")
+    _need(torch.float32, "float32 CUDA tensor", ("kept",), kept)
+    if tuple(kept.shape) != (T, 3):
+        raise ValueError("kept must be [T, 3]")
+    with _on_stream(stream):
+        d_logits_out = _logits_out(d_logits_out, logits)
+    st = lib.lordba_distill_backward(d_loss.data_ptr(), logits.data_ptr(), int(logits.dtype is torch.float32), kept.data_ptr(), ctypes.byref(teacher),
+                                     d_logits_out.data_ptr(), T, V, _stream_handle(logits, stream))
+    if st != 0:
+        raise LordbaError(st, "lordba_distill_backward")
+    return d_logits_out

@@ -1,0 +1,62 @@
+// Products with 4-bit weights: arguments, operands and results, shared by the kernels for few tokens and those for many.
+//
+// The weights' rows are the first operand of v_mfma_f32_16x16x32_f16, the tokens the second, so that a lane's four accumulators are four
+// consecutive columns of y for one token.
+#pragma once
+#include "lordba_dev_util.h"
+#include "lordba_i4.h"
+#include "lordba_results.h"
+
+struct I4Args {
+    const _Float16* x;         // [planes, T, k]: the activations' rows, `k` columns of each plane
+    const uint8_t* codes;      // laid out, see lordba_i4.h
+    const uint16_t *scale, *zero;   // zero: null for 8 everywhere
+    const _Float16* addends;   // gated: [2, T, n], or null
+    _Float16* y;               // [T, n]
+    _Float16* kept;            // gated: [2, T, n], or null
+    int64_t T, k, n;
+    int32_t blocks, plane_blocks;   // of 128 columns: in all, of a plane
+    int32_t tiles;             // blocks of 16 rows of a half
+    int32_t groups;            // forward: along a row, padding included
+    int32_t shift;             // backward: log2 of the group
+    uint32_t first;            // tile of this launch's first workgroup
+};
+
+namespace {
+
+__device__ __forceinline__ h2 both(uint16_t v) { return as_h2(v * 0x10001u); }
+
+// The eight numbers code - zero of a word, exact in fp16.  With the biased exponent 0x64 a code in the low four bits of a half is 1024 + code, one four
+// bits further up 1024 + 16 code; `z` is 1024 + zero, one for all eight (forward) or one each (backward).
+struct Zero1 {
+    h2 low, high;   // 1024 + zero, -(64 + zero)
+    __device__ __forceinline__ explicit Zero1(uint16_t bits) : low(both(bits)), high(h2{static_cast<_Float16>(960), static_cast<_Float16>(960)} - both(bits)) {}
+    __device__ __forceinline__ h2 low_of(int) const { return low; }
+    __device__ __forceinline__ h2 high_of(int) const { return high; }
+};
+struct Zero8 {
+    u4 z;
+    __device__ __forceinline__ h2 low_of(int p) const { return as_h2(z[p]); }
+    __device__ __forceinline__ h2 high_of(int p) const { return h2{static_cast<_Float16>(960), static_cast<_Float16>(960)} - as_h2(z[p]); }
+};
+template <class Z>
+__device__ __forceinline__ h8 operand(uint32_t w, const Z& z) {
+    const h2 sixteenth = {static_cast<_Float16>(0.0625f), static_cast<_Float16>(0.0625f)};
+    auto low = [&](uint32_t v, int p) { return as_h2((v & 0x000F000Fu) | 0x64006400u) - z.low_of(p); };
+    auto high = [&](uint32_t v, int p) { return __builtin_elementwise_fma(as_h2((v & 0x00F000F0u) | 0x64006400u), sixteenth, z.high_of(p)); };
+    const h2 a = low(w, 0), b = high(w, 1), c = low(w >> 8, 2), d = high(w >> 8, 3);
+    return h8{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
+}
+
+__device__ __forceinline__ f4 mfma(h8 a, h8 b, f4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
+
+// For the backward pass: what passes the range of fp16 is kept as its largest number, a NaN as one.
+__device__ __forceinline__ _Float16 kept_half(float v) { return static_cast<_Float16>(v != v ? v : fminf(fmaxf(v, -65504.f), 65504.f)); }
+
+__device__ __forceinline__ float silu(float v) { return v * __builtin_amdgcn_rcpf(1.f + __expf(-v)); }
+
+}  // namespace
+
+// The launches; arguments have been checked.
+lordba_status lordba_i4_few(const I4Args& a, int64_t group, bool gated, bool backward, hipStream_t stream);
+lordba_status lordba_i4_many(const I4Args& a, int64_t group, bool gated, bool backward, hipStream_t stream);

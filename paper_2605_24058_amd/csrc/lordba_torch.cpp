@@ -450,11 +450,154 @@ PyObject* dropout(PyObject*, PyObject* const* a, Py_ssize_t n) {
     END_HANDLE_TH_ERRORS
 }
 
+// ---- 4-bit projections, learning from a teacher.
+struct WeightsI4 {   // the named tuple of the binding: codes, scale, zero or None, rows, cols, group, halves, transposed
+    const at::Tensor *codes, *scale, *zero;
+    int64_t rows, cols, group;
+    bool read(PyObject* o, int halves, bool transposed) {
+        if (!PyTuple_Check(o) || PyTuple_GET_SIZE(o) != 8) return false;
+        PyObject* const z = PyTuple_GET_ITEM(o, 2);
+        codes = plain(PyTuple_GET_ITEM(o, 0), at::kByte), scale = plain(PyTuple_GET_ITEM(o, 1), kF16), zero = z == Py_None ? nullptr : plain(z, kF16);
+        if (!codes || !scale || (!zero && z != Py_None)) return false;
+        int64_t v[4];
+        for (int i = 0; i < 4; ++i) {
+            PyObject* const n = PyTuple_GET_ITEM(o, 3 + i);
+            if (!PyLong_CheckExact(n)) return false;
+            v[i] = PyLong_AsLongLong(n);
+            if (PyErr_Occurred()) { PyErr_Clear(); return false; }
+        }
+        rows = v[0], cols = v[1], group = v[2];
+        if (v[3] != halves || PyTuple_GET_ITEM(o, 7) != (transposed ? Py_True : Py_False)) return false;
+        const int64_t n = static_cast<int64_t>(lordba_i4_scale_count(rows, cols, group, halves, transposed));
+        return n > 0 && codes->numel() == static_cast<int64_t>(lordba_i4_code_bytes(rows, cols, halves, transposed)) && scale->numel() == n &&
+               (!zero || zero->numel() == n);
+    }
+};
+
+// (x, W, y_out, stream), and the same of the gradient with (g, Wt, ...)
+PyObject* linear_i4_any(PyObject* const* a, Py_ssize_t n, bool backward) {
+    NEED(n == 4 && unwatched() && a[3] == Py_None);
+    const at::Tensor* x = plain(a[0], kF16);
+    WeightsI4 w;
+    NEED(x && x->dim() == 2 && w.read(a[1], 1, backward) && x->size(1) == (backward ? w.rows : w.cols));
+    const int64_t T = x->size(0);
+    void* st;
+    at::Tensor y;
+    NEED(stream_of(a[3], x, &st) && tensor_or_new(a[2], kF16, x, {T, backward ? w.cols : w.rows}, false, &y));
+    const int rc = unlocked(backward ? lordba_linear_i4_backward : lordba_linear_i4, ptr<void>(x), ptr<uint8_t>(w.codes), ptr<void>(w.scale),
+                            ptr<void>(w.zero), ptr<void>(y), T, w.cols, w.rows, w.group, st);
+    return result(y, rc);
+}
+PyObject* linear_i4(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    HANDLE_TH_ERRORS
+    return linear_i4_any(a, n, false);
+    END_HANDLE_TH_ERRORS
+}
+PyObject* linear_i4_backward(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    HANDLE_TH_ERRORS
+    return linear_i4_any(a, n, true);
+    END_HANDLE_TH_ERRORS
+}
+
+// (x, W, addends, save, stream)
+PyObject* gated_i4(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    HANDLE_TH_ERRORS
+    NEED(n == 5 && unwatched() && a[4] == Py_None && (a[3] == Py_True || a[3] == Py_False));
+    const at::Tensor *x = plain(a[0], kF16), *add = a[2] == Py_None ? nullptr : plain(a[2], kF16);
+    WeightsI4 w;
+    NEED(x && (add || a[2] == Py_None) && x->dim() == 2 && w.read(a[1], 2, false) && x->size(1) == w.cols);
+    const int64_t T = x->size(0), F = w.rows / 2;
+    NEED(!add || shaped(add, {2, T, F}));
+    void* st;
+    NEED(stream_of(a[4], x, &st));
+    const at::Tensor h = empty(x, kF16, {T, F});
+    at::Tensor kept;
+    if (a[3] == Py_True) kept = empty(x, kF16, {2, T, F});
+    const int rc = unlocked(lordba_gated_i4, ptr<void>(x), ptr<uint8_t>(w.codes), ptr<void>(w.scale), ptr<void>(w.zero), ptr<void>(add), ptr<void>(h),
+                            kept.defined() ? ptr<void>(kept) : nullptr, T, w.cols, F, w.group, st);
+    return rc == LORDBA_OK && kept.defined() ? pair(h, kept) : result(h, rc);
+    END_HANDLE_TH_ERRORS
+}
+
+// (dh, gate_up, Wt, stream)
+PyObject* gated_i4_backward(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    HANDLE_TH_ERRORS
+    NEED(n == 4 && unwatched() && a[3] == Py_None);
+    const at::Tensor *dh = plain(a[0], kF16), *gu = plain(a[1], kF16);
+    WeightsI4 w;
+    NEED(dh && gu && dh->dim() == 2 && w.read(a[2], 2, true) && 2 * dh->size(1) == w.rows);
+    const int64_t T = dh->size(0), F = dh->size(1);
+    NEED(shaped(gu, {2, T, F}));
+    void* st;
+    NEED(stream_of(a[3], dh, &st));
+    const at::Tensor dx = empty(dh, kF16, {T, w.cols}), dgu = empty(dh, kF16, {2, T, F});
+    const int rc = unlocked(lordba_gated_i4_backward, ptr<void>(dh), ptr<void>(gu), ptr<uint8_t>(w.codes), ptr<void>(w.scale), ptr<void>(w.zero), ptr<void>(dx),
+                            ptr<void>(dgu), T, w.cols, F, w.group, st);
+    return rc == LORDBA_OK ? pair(dx, dgu) : PyLong_FromLong(rc);
+    END_HANDLE_TH_ERRORS
+}
+
+struct Distill {   // what both calls share: logits; top_index, top_logits, labels, temperature, soft, hard
+    const at::Tensor* z;
+    int64_t T, V;
+    int type;
+    lordba_teacher w;
+    bool read(PyObject* logits, PyObject* const* a) {
+        type = LORDBA_F16, z = plain(logits, kF16);
+        if (!z) type = LORDBA_F32, z = plain(logits, kF32);
+        if (!z || z->dim() != 2 || z->size(1) < 1) return false;
+        T = z->size(0), V = z->size(1);
+        const at::Tensor *index = a[0] == Py_None ? nullptr : plain(a[0], kI32), *top = a[1] == Py_None ? nullptr : plain(a[1], z->scalar_type()),
+                         *labels = a[2] == Py_None ? nullptr : plain(a[2], kI32);
+        if ((!index && a[0] != Py_None) || (!top && a[1] != Py_None) || (!labels && a[2] != Py_None) || !index != !top) return false;
+        if (index && (index->dim() != 2 || index->size(0) != T || top->sizes() != index->sizes())) return false;
+        if (labels && !shaped(labels, {T})) return false;
+        w.k = index ? index->size(1) : 0;
+        w.top_index = ptr<int32_t>(index), w.top_logits = ptr<void>(top), w.labels = ptr<int32_t>(labels);
+        return number(a[3], &w.temperature) && number(a[4], &w.soft) && number(a[5], &w.hard);
+    }
+};
+
+// (logits, top_index, top_logits, labels, temperature, soft, hard, d_loss, d_logits_out, stream)
+PyObject* distill(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    HANDLE_TH_ERRORS
+    Distill d;
+    NEED(n == 10 && unwatched() && a[9] == Py_None && d.read(a[0], a + 1));
+    const at::Tensor* weight = a[7] == Py_None ? nullptr : plain(a[7], kF32);
+    NEED((weight && shaped(weight, {d.T})) || (a[7] == Py_None && a[8] == Py_None));
+    void* st;
+    at::Tensor grad, kept;
+    NEED(stream_of(a[9], d.z, &st) && (!weight || tensor_or_new(a[8], d.z->scalar_type(), d.z, d.z->sizes(), false, &grad)));
+    const at::Tensor loss = empty(d.z, kF32, {d.T});
+    if (!weight) kept = empty(d.z, kF32, {d.T, 3});
+    const int rc = unlocked(lordba_distill, ptr<void>(d.z), d.type, &d.w, ptr<float>(weight), ptr<float>(loss), weight ? nullptr : ptr<float>(kept),
+                            weight ? ptr<void>(grad) : nullptr, d.T, d.V, st);
+    return rc == LORDBA_OK ? pair(loss, weight ? grad : kept) : PyLong_FromLong(rc);
+    END_HANDLE_TH_ERRORS
+}
+
+// (d_loss, logits, kept, top_index, top_logits, labels, temperature, soft, hard, d_logits_out, stream)
+PyObject* distill_backward(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    HANDLE_TH_ERRORS
+    Distill d;
+    NEED(n == 11 && unwatched() && a[10] == Py_None && d.read(a[1], a + 3));
+    const at::Tensor *weight = plain(a[0], kF32), *kept = plain(a[2], kF32);
+    NEED(weight && kept && shaped(weight, {d.T}) && shaped(kept, {d.T, 3}));
+    void* st;
+    at::Tensor grad;
+    NEED(stream_of(a[10], d.z, &st) && tensor_or_new(a[9], d.z->scalar_type(), d.z, d.z->sizes(), false, &grad));
+    const int rc = unlocked(lordba_distill_backward, ptr<float>(weight), ptr<void>(d.z), d.type, ptr<float>(kept), &d.w, ptr<void>(grad), d.T, d.V, st);
+    return result(grad, rc);
+    END_HANDLE_TH_ERRORS
+}
+
 #define METHOD(name) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(name)), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {METHOD(forward),        METHOD(forward_multi),        METHOD(forward_batched), METHOD(forward_batched_multi),
                          METHOD(pack_latents),   METHOD(forward_save_t),       METHOD(forward_multi_save_t),
                          METHOD(backward),       METHOD(backward_multi),       METHOD(linear_i8),
                          METHOD(linear_i8_backward), METHOD(gated_i8),           METHOD(gated_i8_backward), METHOD(dropout),
+                         METHOD(linear_i4),      METHOD(linear_i4_backward),   METHOD(gated_i4),        METHOD(gated_i4_backward),
+                         METHOD(distill),        METHOD(distill_backward),
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_lordba_torch", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
