@@ -8,9 +8,6 @@ lordba_status check(int64_t T, int64_t d_in, int64_t d_out, int64_t group) {
     return i4_group(group) ? LORDBA_OK : LORDBA_ERR_VALUE;
 }
 
-// Up to this many tokens the kernel that reads activations straight into registers is used.
-constexpr int64_t kFew = 64;
-
 struct Weights {
     const uint8_t* codes;
     const void *scale, *zero;
@@ -24,9 +21,10 @@ lordba_status product(I4Args a, const Weights& w, const I4Shape& s, int64_t grou
     a.tiles = static_cast<int32_t>(s.tiles / s.row_halves);
     a.groups = static_cast<int32_t>(s.groups);
     a.shift = group == 32 ? 5 : group == 64 ? 6 : 7;
-    a.first = 0;
+    a.aligned = a.k % 8 == 0 && !i8_misaligned(a.x, 16);
     const hipStream_t st = static_cast<hipStream_t>(stream);
-    return a.T <= kFew ? lordba_i4_few(a, group, gated, backward, st) : lordba_i4_many(a, group, gated, backward, st);
+    const I4Kernel kernel = i4_kernel(a.T, a.k, a.blocks, a.n, gated, a.aligned != 0);
+    return kernel == kI4Few ? lordba_i4_few(a, group, gated, backward, st) : lordba_i4_many(a, kernel, group, gated, backward, st);
 }
 
 size_t bytes_of(const I4Shape& s) { return static_cast<size_t>(s.tiles) * static_cast<size_t>(s.blocks) * 1024; }

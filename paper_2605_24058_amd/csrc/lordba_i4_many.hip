@@ -20,45 +20,56 @@ __device__ __forceinline__ Tile tile_of(uint32_t id, uint32_t nc, uint32_t nt) {
     return {in / size, g * kTogether + in % size};
 }
 
-// A workgroup owns 16 CB WC weight rows (gated: half of them gate's, half up's) and 16 TB WT tokens, each of its WC x WT waves CB x TB blocks of 16 x 16.
-// A step is a block of 128 columns.  The activations of a step lie in LDS, of which two steps' are held, rows of 256 bytes with their 16-byte piece p
-// at place p ^ (row mod 16): sixteen lanes that read one piece of sixteen rows cover all banks.  The weights come from memory straight into the
-// registers of the waves that multiply them, a step ahead, and become fp16 there: their scale is multiplied on before the product, which rounds each weight once
-// (half a step, 2^-11 of it; scales taken out of the sums instead, as for few tokens, would be exact, but take a multiplication for every accumulator and group).
-template <int CB, int TB, int WC, int WT, int S, bool ZERO, bool GATED>
-__global__ __launch_bounds__(64 * WC * WT) void lordba_i4_many_kernel(I4Args a) {
+typedef float sums16 __attribute__((ext_vector_type(16)));
+
+// A workgroup owns 32 CP WC weight rows (gated: half of them gate's, half up's) and 32 TB WT tokens, each of its WC x WT waves CP x TB blocks of 32 x 32 by
+// v_mfma_f32_32x32x16_f16.  A step is a block of 128 columns, eight products deep.
+// Activations.  Those of a step lie in LDS, of which two steps' are held, rows of 256 bytes with their 16-byte piece p at place p ^ (row mod 16): sixteen
+// lanes that read one piece of sixteen rows cover all banks.
+// Weights.  They come from memory straight into the registers of the waves that multiply them, a step ahead.  A pair of 16-row blocks is a 32-row operand: lane
+// 32 h + 16 b + r takes from block b what lanes 16 (2 c + h) + r hold (lordba_i4.h), which is row r's columns 32 m + 16 c + 8 h .. + 7 for m = 0 .. 3 and c = 0, 1.
+// They become fp16 in the registers, their scale multiplied on before the product, which rounds each weight once (half a step, 2^-11 of it; scales taken out of
+// the sums instead, as for few tokens, would be exact, but take a multiplication for every accumulator and group).
+// While the products of one depth run, the operands of the next are read from LDS and made from the codes.  The barrier stands one depth before a step's
+// end: everybody has then read the step's activations, and the next step's have landed.
+template <int CP, int TB, int WC, int WT, int WK, int S, bool ZERO, bool GATED, bool BY_REGISTERS>
+__global__ __launch_bounds__(64 * WC * WT * WK, 2) void lordba_i4_many_kernel(I4Args a) {
     constexpr bool BWD = S == 0;
-    constexpr int P = GATED ? 2 : 1, NW = WC * WT, CT = CB / P, kTiles = CT * WC, kTokens = 16 * TB * WT;   // kTiles: blocks of a half
-    constexpr int kGroups = BWD ? (16 * kTiles + 31) / 32 : 0;   // most groups across a workgroup's rows
-    constexpr uint32_t kX = kTokens * 256u, kS = kGroups * 256u, kBuffer = kX + kS * (ZERO ? 2 : 1);
-    static_assert(CT % 2 == 0 && !(GATED && BWD), "pairs of blocks");
-    extern __shared__ int8_t lds[];
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 15, q = lane >> 4;
-    const int wc = wave % WC, wt = wave / WC;
-    const Tile at = tile_of(a.first + blockIdx.x, static_cast<uint32_t>((a.tiles + kTiles - 1) / kTiles), static_cast<uint32_t>((a.T + kTokens - 1) / kTokens));
-    const int first_tile = static_cast<int>(at.c) * kTiles, tile0 = first_tile + wc * CT;
+    constexpr int P = GATED ? 2 : 1, NW = WC * WT, PW = CP / P, kPairs = PW * WC, kTokens = 32 * TB * WT;   // kPairs: row pairs of a half
+    constexpr int kEach = BWD ? (kPairs + 3) / 4 : 0;   // KiB for the scales of the groups across a workgroup's rows
+    constexpr uint32_t kX = kTokens * 256u, kS = kEach * 1024u, kBuffer = kX + kS * (ZERO ? 2 : 1);
+    static_assert(CP % P == 0 && !(GATED && BWD), "");
+    extern __shared__ int8_t all_lds[];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n = lane & 31, h = lane >> 5;
+    const int wk = wave / NW, wi = wave % NW, wc = wi % WC, wt = wi / WC, pairs = a.tiles / 2;
+    const Tile at = tile_of(a.first + blockIdx.x, static_cast<uint32_t>((pairs + kPairs - 1) / kPairs), static_cast<uint32_t>((a.T + kTokens - 1) / kTokens));
+    int8_t* const lds = all_lds + wk * 2 * kBuffer;
+    const int steps = (a.blocks + WK - 1) / WK;
+    const int first_pair = static_cast<int>(at.c) * kPairs, pair0 = first_pair + wc * PW;
     const int64_t first_token = static_cast<int64_t>(at.t) * kTokens;
 
-    const u4* code[CB];
-    const uint16_t *scale[CB], *zero[CB];
-    uint32_t s_at[CB];   // backward: where in a buffer the scales of the block's group start
-    const int group0 = BWD ? static_cast<int>(i4_row(first_tile, 0) >> a.shift) : 0;
+    const u4* code[CP];
+    const uint16_t *scale[CP], *zero[CP];
+    uint32_t s_at[CP];   // backward: where in a buffer the scales of the pair's group start
+    const int group0 = BWD ? (32 * first_pair) >> a.shift : 0;
 #pragma unroll
-    for (int i = 0; i < CB; ++i) {
-        const int64_t tile = min(tile0 + i % CT, a.tiles - 1) + (i / CT) * a.tiles;
-        code[i] = reinterpret_cast<const u4*>(a.codes) + tile * a.blocks * 64 + lane;
-        scale[i] = BWD ? nullptr : a.scale + tile * a.groups * 16 + r;
-        zero[i] = BWD || !ZERO ? nullptr : a.zero + tile * a.groups * 16 + r;
-        s_at[i] = BWD ? static_cast<uint32_t>((i4_row(tile, 0) >> a.shift) - group0) * 256u : 0;
+    for (int i = 0; i < CP; ++i) {
+        const int pair = min(pair0 + i % PW, pairs - 1) + (i / PW) * pairs;
+        const int64_t tile = 2 * static_cast<int64_t>(pair) + (n >> 4);
+        code[i] = reinterpret_cast<const u4*>(a.codes) + tile * a.blocks * 64 + 16 * h + (n & 15);
+        scale[i] = BWD ? nullptr : a.scale + tile * a.groups * 16 + (n & 15);
+        zero[i] = BWD || !ZERO ? nullptr : a.zero + tile * a.groups * 16 + (n & 15);
+        s_at[i] = BWD ? static_cast<uint32_t>(((32 * pair) >> a.shift) - group0) * 256u : 0;
     }
     struct Weights {
-        u4 c[CB];
-        uint16_t s[BWD ? 1 : CB][BWD ? 1 : S], z[!BWD && ZERO ? CB : 1][BWD ? 1 : S];
+        u4 c[CP][2];
+        uint16_t s[BWD ? 1 : CP][BWD ? 1 : S], z[!BWD && ZERO ? CP : 1][BWD ? 1 : S];
     };
-    auto load_weights = [&](int b, Weights& w) {
+    auto load_weights = [&](int b, Weights& w) __attribute__((always_inline)) {
 #pragma unroll
-        for (int i = 0; i < CB; ++i) {
-            w.c[i] = code[i][static_cast<int64_t>(b) * 64];
+        for (int i = 0; i < CP; ++i) {
+            w.c[i][0] = code[i][static_cast<int64_t>(b) * 64];
+            w.c[i][1] = code[i][static_cast<int64_t>(b) * 64 + 32];
             if constexpr (!BWD) {
 #pragma unroll
                 for (int s = 0; s < S; ++s) {
@@ -68,148 +79,283 @@ __global__ __launch_bounds__(64 * WC * WT) void lordba_i4_many_kernel(I4Args a) 
             }
         }
     };
-    // The activations of step b, and the scales that go with them.  Whole steps of aligned rows go straight into LDS.
-    const bool aligned = a.k % 8 == 0 && (reinterpret_cast<uintptr_t>(a.x) & 15) == 0;
+    // The activations of step b, and the scales that go with them, straight into LDS, request by request; pieces behind the rows' end hold what is in front of it
+    // and are cleared when they have landed (a NaN among them would pass the weights of 0 there).  Rows that do not consist of aligned pieces (BY_REGISTERS) are
+    // requested into registers and stored, moved into place at their end, before the barrier that the step waits for.
     const uint32_t base = static_cast<uint32_t>(reinterpret_cast<uintptr_t>(lds));
-    auto stage = [&](int b, uint32_t buffer) {
-        const int plane = b >= a.plane_blocks ? 1 : 0;
-        const int64_t c0 = static_cast<int64_t>(b - plane * a.plane_blocks) * kI4Columns;
-        const _Float16* const x = a.x + plane * a.T * a.k;
-        if (aligned && c0 + kI4Columns <= a.k) {
+    constexpr int kLoads = kTokens / 4 / NW;
+    static_assert(kTokens / 4 % NW == 0, "whole loads per wave");
+    const int32_t last_row = static_cast<int32_t>(min<int64_t>(a.T - 1 - first_token, kTokens - 1));
+    const int32_t row0 = 4 * wi + (lane >> 4);
+    u4 held[BY_REGISTERS ? kLoads : 1];
+    // (of the WK blocks of a step this wave has the wk-th; where there is none, the last stands in, behind the rows' end altogether)
+    auto block_of = [&](int step) __attribute__((always_inline)) { return min(step * WK + wk, a.blocks - 1); };
+    auto column_of = [&](int b) __attribute__((always_inline)) { return (b >= a.plane_blocks ? b - a.plane_blocks : b) * static_cast<int32_t>(kI4Columns); };
+    auto end_of = [&](int step, int w) __attribute__((always_inline)) {   // of the w-th block of a step: its columns
+        const int b = step * WK + w;
+        return b < a.blocks ? static_cast<int32_t>(a.k) - column_of(b) : 0;
+    };
+    auto piece_of = [&](int i) __attribute__((always_inline)) { return 8 * ((lane & 15) ^ ((row0 + 4 * NW * i) & 15)); };   // (in halves)
+    auto request = [&](int step, uint32_t buffer, int i) __attribute__((always_inline)) {
+        const int b = block_of(step);
+        const int32_t c0 = column_of(b), k = static_cast<int32_t>(a.k);
+        const _Float16* const x = a.x + ((b >= a.plane_blocks ? a.T : 0) + first_token) * a.k;
+        // (a tile's rows span less than 4 GiB: what the launch sees to)
+        const uint32_t at = (static_cast<uint32_t>(min(row0 + 4 * NW * i, last_row)) * static_cast<uint32_t>(k) + min(c0 + piece_of(i), k - 8)) * 2u;
+        if constexpr (BY_REGISTERS) held[i] = load16_any(reinterpret_cast<const char*>(x) + at);
+        else load16_to_lds_from(base + buffer + (wi + NW * i) * 1024u, x, at);
+    };
+    auto request_scales = [&](int step, uint32_t buffer) __attribute__((always_inline)) {
+        if constexpr (BWD) {   // (a place for each group there may be; groups behind the last are not read by anybody)
+            constexpr int kAll = kEach * (ZERO ? 2 : 1);
+            static_assert(kAll % NW == 0 || NW % kAll == 0, "a wave for each KiB, or several, or several for each");
 #pragma unroll
-            for (int i = 0; i < kTokens / 4 / NW; ++i) {
-                const int row = 4 * (wave + NW * i) + q;
-                load16_to_lds<false>(base + buffer + (wave + NW * i) * 1024u, x + min(first_token + row, a.T - 1) * a.k + c0 + 8 * (r ^ (row & 15)));
-            }
-        } else {
-#pragma unroll 4
-            for (int i = 0; i < kTokens / 4 / NW; ++i) {
-                const int row = 4 * (wave + NW * i) + q;
-                const u4 v = load_part(x + min(first_token + row, a.T - 1) * a.k, c0 + 8 * (r ^ (row & 15)), a.k);
-                *reinterpret_cast<u4*>(lds + buffer + (wave + NW * i) * 1024u + 16 * lane) = v;
-            }
-        }
-        if constexpr (BWD) {   // (rows of groups that the matrix does not have stay unread)
-            const int group = threadIdx.x >> 4, piece = threadIdx.x & 15;
-            if (group < kGroups && group0 + group <= static_cast<int>((a.n - 1) >> a.shift)) {
-                const int64_t from = (static_cast<int64_t>(group0 + group) * a.blocks + b) * kI4Columns + 8 * piece;
-                *reinterpret_cast<u4*>(lds + buffer + kX + group * 256 + 16 * piece) = load16(a.scale + from);
-                if constexpr (ZERO) *reinterpret_cast<u4*>(lds + buffer + kX + kS + group * 256 + 16 * piece) = load16(a.zero + from);
+            for (int j = 0; j < kAll; j += NW) {
+                const int p = (wi + j) % kAll, part = p % kEach, group = min(group0 + 4 * part + (lane >> 4), static_cast<int>((a.n - 1) >> a.shift));
+                load16_to_lds<false>(base + buffer + kX + p * 1024u,
+                                     (p >= kEach ? a.zero : a.scale) + (static_cast<int64_t>(group) * a.blocks + block_of(step)) * kI4Columns + 8 * (lane & 15));
             }
         }
     };
-    static_assert(!BWD || kGroups * 16 <= 64 * NW, "a thread for each piece");
-    f4 acc[CB][TB];
+    auto stage = [&](int step, uint32_t buffer) __attribute__((always_inline)) {
 #pragma unroll
-    for (int i = 0; i < CB; ++i)
+        for (int i = 0; i < kLoads; ++i) request(step, buffer, i);
+        request_scales(step, buffer);
+    };
+    auto store_held = [&](int step, uint32_t buffer) __attribute__((always_inline)) {
+        if constexpr (BY_REGISTERS) {
+            const int32_t end = end_of(step, wk);
 #pragma unroll
-        for (int j = 0; j < TB; ++j) acc[i][j] = f4{0.f, 0.f, 0.f, 0.f};
-    const int8_t* const mine = lds + (wt * TB * 16 + r) * 256;
-    auto multiply = [&](uint32_t buffer, const Weights& v) {
-#pragma unroll
-        for (int m = 0; m < 4; ++m) {
-            h8 x[TB], w[CB];
-#pragma unroll
-            for (int j = 0; j < TB; ++j) x[j] = as_h8(*reinterpret_cast<const u4*>(mine + buffer + j * 4096 + 16 * ((4 * m + q) ^ r)));
-#pragma unroll
-            for (int i = 0; i < CB; ++i) {
-                if constexpr (BWD) {
-                    const int8_t* const s = lds + buffer + kX + s_at[i] + 64 * m + 16 * q;
-                    if constexpr (ZERO) w[i] = operand(v.c[i][m], Zero8{*reinterpret_cast<const u4*>(s + kS)});
-                    else w[i] = operand(v.c[i][m], Zero1(kZero8));
-                    w[i] = w[i] * as_h8(*reinterpret_cast<const u4*>(s));
-                } else {
-                    constexpr int kEach = 4 / (S ? S : 1);
-                    w[i] = operand(v.c[i][m], Zero1(ZERO ? v.z[i][m / kEach] : kZero8));
-                    const h2 s = both(v.s[i][m / kEach]);
-                    w[i] = w[i] * h8{s[0], s[0], s[0], s[0], s[0], s[0], s[0], s[0]};
-                }
+            for (int i = 0; i < kLoads; ++i) {
+                const int32_t over = piece_of(i) - (end - 8);
+                if (end < kI4Columns && over > 0) held[i] = drop_halves(held[i], over);
+                *reinterpret_cast<u4*>(lds + buffer + (wi + NW * i) * 1024u + 16 * lane) = held[i];
             }
-#pragma unroll
-            for (int i = 0; i < CB; ++i)
-#pragma unroll
-                for (int j = 0; j < TB; ++j) acc[i][j] = mfma(w[i], x[j], acc[i][j]);
         }
     };
-    // What has been requested has landed, and everybody has read the buffer that comes next.
-    auto meet = [] {
+    // Pieces of a step behind the rows' end, when everything has landed; whoever requested a piece clears it.
+    auto clear_end = [&](int step, uint32_t buffer) __attribute__((always_inline)) {
+        if constexpr (!BY_REGISTERS) {
+            int32_t least = kI4Columns;
+#pragma unroll
+            for (int w = 0; w < WK; ++w) least = min(least, end_of(step, w));
+            if (least >= kI4Columns) return;
+            const int32_t end = end_of(step, wk);
+#pragma unroll
+            for (int i = 0; i < kLoads; ++i)
+                if (piece_of(i) >= end) *reinterpret_cast<u4*>(lds + buffer + (wi + NW * i) * 1024u + 16 * lane) = u4{0u, 0u, 0u, 0u};
+            __syncthreads();
+        }
+    };
+    sums16 acc[CP][TB];
+#pragma unroll
+    for (int i = 0; i < CP; ++i)
+#pragma unroll
+        for (int j = 0; j < TB; ++j)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.f;
+    // operands of depth d = 2 m + c of a step
+    const int8_t* const mine = lds + (wt * TB * 32 + n) * 256;
+    h8 x[2][TB], w[2][CP];
+    const uint32_t exp = exponent();
+    auto operands = [&](auto depth, uint32_t buffer, const Weights& v) __attribute__((always_inline)) {
+        constexpr int d = depth.value, m = d >> 1, c = d & 1, set = d & 1;
+#pragma unroll
+        for (int j = 0; j < TB; ++j) x[set][j] = as_h8(*reinterpret_cast<const u4*>(mine + buffer + j * 8192 + 16 * ((2 * d + h) ^ (n & 15))));
+#pragma unroll
+        for (int i = 0; i < CP; ++i) {
+            if constexpr (BWD) {
+                const int8_t* const s = lds + buffer + kX + s_at[i] + 32 * d + 16 * h;
+                if constexpr (ZERO) w[set][i] = operand(v.c[i][c][m], Zero8{*reinterpret_cast<const u4*>(s + kS)}, exp);
+                else w[set][i] = operand(v.c[i][c][m], Zero1(kZero8), exp);
+                w[set][i] = w[set][i] * as_h8(*reinterpret_cast<const u4*>(s));
+            } else {
+                constexpr int g = m * (S ? S : 1) / 4;
+                w[set][i] = operand(v.c[i][c][m], Zero1(ZERO ? v.z[i][g] : kZero8), exp);
+                const h2 s = both(v.s[i][g]);
+                w[set][i] = w[set][i] * h8{s[0], s[0], s[0], s[0], s[0], s[0], s[0], s[0]};
+            }
+        }
+    };
+    auto multiply = [&](auto set) __attribute__((always_inline)) {
+#pragma unroll
+        for (int i = 0; i < CP; ++i)
+#pragma unroll
+            for (int j = 0; j < TB; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(w[set.value][i], x[set.value][j], acc[i][j], 0, 0, 0);
+    };
+    // between every few products some of the next operands' work
+    auto weave = []() __attribute__((always_inline)) {
+#pragma unroll
+        for (int i = 0; i < CP * TB; ++i) {
+            __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);
+            __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+            __builtin_amdgcn_sched_group_barrier(0x2, 16 * CP / (CP * TB), 0);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+    };
+    // What has been requested has landed, and everybody has read what was in the other buffer.
+    auto meet = []() __attribute__((always_inline)) {
         asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");
     };
-    Weights now;
-    stage(0, 0);
-    load_weights(0, now);
-    uint32_t buffer = 0;
-    for (int b = 0; b < a.blocks; ++b) {
-        meet();
-        Weights next = now;
-        if (b + 1 < a.blocks) {
-            stage(b + 1, kBuffer - buffer);
-            load_weights(b + 1, next);
-        }
-        multiply(buffer, now);
-        now = next;
-        buffer = kBuffer - buffer;
-    }
-    // A lane has eight consecutive columns of a token in a pair of blocks.
-    auto finish = [&](auto whole, auto odd) {
-        constexpr bool FULL = whole.value, ODD = odd.value;
-        const int64_t plane = a.T * a.n;
+    // (the copy is made here, not behind the loads into `next`: their arrival would be waited for with it)
+    auto settle = [](Weights& v) __attribute__((always_inline)) {
 #pragma unroll
-        for (int i = 0; i < CT; i += 2) {
-            const int64_t c = i4_row(tile0 + i, 4 * q);
-            if (!FULL && c >= a.n) continue;
+        for (int i = 0; i < CP; ++i) {
+            asm volatile("" : "+v"(v.c[i][0]), "+v"(v.c[i][1]));
+            if constexpr (!BWD) {
 #pragma unroll
-            for (int j = 0; j < TB; ++j) {
-                const int64_t t = first_token + (wt * TB + j) * 16 + r;
-                if (!FULL && t >= a.T) continue;
-                float v[P][8];
-#pragma unroll
-                for (int p = 0; p < P; ++p)
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) v[p][e] = acc[p * CT + i + (e >> 2)][j][e & 3];
-                if constexpr (GATED) {
-                    if (a.addends) {
-#pragma unroll
-                        for (int p = 0; p < P; ++p) {
-                            const h8 add = as_h8(load8<FULL>(a.addends + p * plane + t * a.n, c, a.n));
-#pragma unroll
-                            for (int e = 0; e < 8; ++e) v[p][e] += static_cast<float>(add[e]);
-                        }
-                    }
-                    if (a.kept) {
-#pragma unroll
-                        for (int p = 0; p < P; ++p) {
-                            if constexpr (ODD) store8_odd<true>(a.kept + p * plane + t * a.n + c, v[p]);
-                            else store8<FULL, false, true>(a.kept + p * plane + t * a.n, c, a.n, v[p]);
-                        }
-                    }
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) v[0][e] = silu(v[0][e]) * v[1][e];
+                for (int s = 0; s < S; ++s) {
+                    asm volatile("" : "+v"(v.s[i][s]));
+                    if constexpr (ZERO) asm volatile("" : "+v"(v.z[i][s]));
                 }
-                if constexpr (ODD) store8_odd<false>(a.y + t * a.n + c, v[0]);
-                else store8<FULL, false, false>(a.y + t * a.n, c, a.n, v[0]);
             }
         }
     };
-    const bool full = (first_tile + kTiles) * 16 <= a.n && first_token + kTokens <= a.T;
-    if (!full) finish(std::false_type{}, std::false_type{});
-    else if ((a.n & 1) || ((reinterpret_cast<uintptr_t>(a.y) | reinterpret_cast<uintptr_t>(a.kept)) & 2)) finish(std::true_type{}, std::true_type{});
-    else finish(std::true_type{}, std::false_type{});
+    Weights now, next;
+    stage(0, 0);
+    load_weights(block_of(0), now);
+    store_held(0, 0);
+    meet();
+    clear_end(0, 0);
+    stage(min(1, steps - 1), kBuffer);
+    load_weights(block_of(min(1, steps - 1)), next);
+    operands(std::integral_constant<int, 0>{}, 0, now);
+    uint32_t buffer = 0;
+    for (int step = 0; step < steps; ++step) {
+        auto depth = [&](auto d) __attribute__((always_inline)) {
+            operands(std::integral_constant<int, d.value + 1>{}, buffer, now);
+            multiply(std::integral_constant<int, d.value & 1>{});
+            weave();
+        };
+        depth(std::integral_constant<int, 0>{});
+        depth(std::integral_constant<int, 1>{});
+        depth(std::integral_constant<int, 2>{});
+        depth(std::integral_constant<int, 3>{});
+        depth(std::integral_constant<int, 4>{});
+        depth(std::integral_constant<int, 5>{});
+        depth(std::integral_constant<int, 6>{});
+        // (the operands of depth 7 are made above, not behind the barrier)
+#pragma unroll
+        for (int i = 0; i < CP; ++i) asm volatile("" : "+v"(w[1][i]));
+        // (Behind the last step what is there is requested once more, operands are made of it, and nobody multiplies them.)
+        const int next_step = min(step + 1, steps - 1), behind = min(step + 2, steps - 1);
+        store_held(next_step, kBuffer - buffer);
+        meet();
+        clear_end(next_step, kBuffer - buffer);
+        now = next;
+        settle(now);
+        load_weights(block_of(behind), next);
+        request_scales(behind, buffer);
+        const uint32_t freed = buffer;
+        buffer = kBuffer - buffer;
+        operands(std::integral_constant<int, 0>{}, buffer, now);
+#pragma unroll
+        for (int l = 0; l < kLoads; ++l) request(behind, freed, l);
+        multiply(std::integral_constant<int, 1>{});
+        weave();
+    }
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // (nothing is on its way into LDS when the workgroup ends, or takes it for its sums)
+
+    // Results of a block, of both halves where there are two: a lane has two times eight consecutive columns of a token.
+    const int64_t plane = a.T * a.n;
+    auto finish = [&](auto whole, auto odd, int i, int j, const sums16 (&sum)[P]) __attribute__((always_inline)) {
+        constexpr bool FULL = whole.value, ODD = odd.value;
+        const int64_t t = first_token + (wt * TB + j) * 32 + n;
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+            const int64_t c = 32 * static_cast<int64_t>(pair0 + i) + 16 * u + 8 * h;
+            if (!FULL && (c >= a.n || t >= a.T)) continue;
+            float v[P][8];
+#pragma unroll
+            for (int p = 0; p < P; ++p)
+#pragma unroll
+                for (int e = 0; e < 8; ++e) v[p][e] = sum[p][4 * (u + 2 * (e >> 2)) + (e & 3)];
+            if constexpr (GATED) {
+                if (a.addends) {
+#pragma unroll
+                    for (int p = 0; p < P; ++p) {
+                        const h8 add = as_h8(load8<FULL>(a.addends + p * plane + t * a.n, c, a.n));
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) v[p][e] += static_cast<float>(add[e]);
+                    }
+                }
+                if (a.kept) {
+#pragma unroll
+                    for (int p = 0; p < P; ++p) {
+                        if constexpr (ODD) store8_odd<true, 32>(a.kept + p * plane + t * a.n + c, v[p]);
+                        else store8<FULL, false, true>(a.kept + p * plane + t * a.n, c, a.n, v[p]);
+                    }
+                }
+#pragma unroll
+                for (int e = 0; e < 8; ++e) v[0][e] = silu(v[0][e]) * v[1][e];
+            }
+            if constexpr (ODD) store8_odd<false, 32>(a.y + t * a.n + c, v[0]);
+            else store8<FULL, false, false>(a.y + t * a.n, c, a.n, v[0]);
+        }
+    };
+    const bool full = 32 * static_cast<int64_t>(first_pair + kPairs) <= a.n && first_token + kTokens <= a.T;
+    const bool odd = (a.n & 1) || ((reinterpret_cast<uintptr_t>(a.y) | reinterpret_cast<uintptr_t>(a.kept)) & 2) != 0;
+    if constexpr (WK == 1) {
+        auto all = [&](auto whole, auto is_odd) __attribute__((always_inline)) {
+#pragma unroll
+            for (int i = 0; i < PW; ++i)
+#pragma unroll
+                for (int j = 0; j < TB; ++j) {
+                    sums16 sum[P];
+#pragma unroll
+                    for (int p = 0; p < P; ++p) sum[p] = acc[p * PW + i][j];
+                    finish(whole, is_odd, i, j, sum);
+                }
+        };
+        if (!full) all(std::false_type{}, std::false_type{});
+        else if (odd) all(std::true_type{}, std::true_type{});
+        else all(std::true_type{}, std::false_type{});
+    } else {
+        // The sums of the WK parts are joined through LDS, in their order, block by block; the parts share the blocks.
+        f4* const parts = reinterpret_cast<f4*>(all_lds);
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < CP; ++i)
+#pragma unroll
+            for (int j = 0; j < TB; ++j)
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    parts[((wave * CP + i) * TB + j) * 256 + e * 64 + lane] = f4{acc[i][j][4 * e], acc[i][j][4 * e + 1], acc[i][j][4 * e + 2], acc[i][j][4 * e + 3]};
+        __syncthreads();
+        for (int o = wk; o < PW * TB; o += WK) {
+            sums16 sum[P];
+#pragma unroll
+            for (int p = 0; p < P; ++p)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    f4 s = parts[((wi * CP + p * PW) * TB + o) * 256 + e * 64 + lane];
+#pragma unroll
+                    for (int w = 1; w < WK; ++w) s += parts[(((w * NW + wi) * CP + p * PW) * TB + o) * 256 + e * 64 + lane];
+#pragma unroll
+                    for (int f = 0; f < 4; ++f) sum[p][4 * e + f] = s[f];
+                }
+            const int i = o / TB, j = o % TB;
+            if (!full) finish(std::false_type{}, std::false_type{}, i, j, sum);
+            else if (odd) finish(std::true_type{}, std::true_type{}, i, j, sum);
+            else finish(std::true_type{}, std::false_type{}, i, j, sum);
+        }
+    }
 }
 
-template <int CB, int TB, int WC, int WT, int S, bool ZERO, bool GATED>
+template <int CP, int TB, int WC, int WT, int WK, int S, bool ZERO, bool GATED, bool BY_REGISTERS>
 lordba_status many_launch(I4Args a, hipStream_t stream) {
-    constexpr int kTiles = CB / (GATED ? 2 : 1) * WC, kTokens = 16 * TB * WT;
-    constexpr size_t kScales = S == 0 ? (16 * kTiles + 31) / 32 * 256 * (ZERO ? 2 : 1) : 0, kLds = 2 * (kTokens * 256 + kScales);
+    constexpr int kPairs = CP / (GATED ? 2 : 1) * WC, kTokens = 32 * TB * WT;
+    constexpr size_t kScales = S == 0 ? (kPairs + 3) / 4 * 1024 * (ZERO ? 2 : 1) : 0, kRing = 2 * WK * (kTokens * 256 + kScales);
+    constexpr size_t kSums = WK == 1 ? 0 : static_cast<size_t>(WK) * WC * WT * CP * TB * 4096, kLds = kRing > kSums ? kRing : kSums;
     static_assert(kLds <= kLdsBytes, "LDS of a compute unit");
     if (kLds > 64 * 1024) {   // (once for a device: more LDS than a launch gets unasked)
         static std::atomic<uint64_t> asked{0};
         int device = 0;
         if (hipGetDevice(&device) != hipSuccess || device < 0 || device >= 64) return LORDBA_ERR_NO_DEVICE;
         if (!(asked.load(std::memory_order_relaxed) >> device & 1)) {
-            if (hipFuncSetAttribute(reinterpret_cast<const void*>(lordba_i4_many_kernel<CB, TB, WC, WT, S, ZERO, GATED>),
+            if (hipFuncSetAttribute(reinterpret_cast<const void*>(lordba_i4_many_kernel<CP, TB, WC, WT, WK, S, ZERO, GATED, BY_REGISTERS>),
                                     hipFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(kLds)) != hipSuccess) {
                 (void)hipGetLastError();
                 return LORDBA_ERR_LAUNCH;
@@ -217,30 +363,44 @@ lordba_status many_launch(I4Args a, hipStream_t stream) {
             asked.fetch_or(static_cast<uint64_t>(1) << device, std::memory_order_relaxed);
         }
     }
-    const int64_t n = static_cast<int64_t>((a.tiles + kTiles - 1) / kTiles) * ((a.T + kTokens - 1) / kTokens);
-    if (n > INT32_MAX / 512) return LORDBA_ERR_DIM;
-    hipLaunchKernelGGL((lordba_i4_many_kernel<CB, TB, WC, WT, S, ZERO, GATED>), dim3(static_cast<unsigned>(n)), dim3(64 * WC * WT), kLds, stream, a);
-    return i8_launched();
+    const int64_t n = static_cast<int64_t>((a.tiles / 2 + kPairs - 1) / kPairs) * ((a.T + kTokens - 1) / kTokens);
+    constexpr int64_t kMost = (static_cast<int64_t>(1) << 31) / (64 * WC * WT * WK);   // (a launch counts threads in 32 bits)
+    if (n > INT32_MAX) return LORDBA_ERR_DIM;
+    for (int64_t first = 0; first < n; first += kMost) {
+        a.first = static_cast<uint32_t>(first);
+        hipLaunchKernelGGL((lordba_i4_many_kernel<CP, TB, WC, WT, WK, S, ZERO, GATED, BY_REGISTERS>), dim3(static_cast<unsigned>(std::min(kMost, n - first))), dim3(64 * WC * WT * WK),
+                           kLds, stream, a);
+        const lordba_status st = i8_launched();
+        if (st != LORDBA_OK) return st;
+    }
+    return LORDBA_OK;
 }
 
 template <int S, bool ZERO, bool GATED>
-lordba_status many(const I4Args& a, hipStream_t stream) {
-    const int64_t large = static_cast<int64_t>((a.tiles * (GATED ? 2 : 1) + 15) / 16) * ((a.T + 255) / 256);
-    if (large >= 192) return many_launch<4, 8, 4, 2, S, ZERO, GATED>(a, stream);
-    return many_launch<4, 4, 2, 2, S, ZERO, GATED>(a, stream);
+lordba_status many(const I4Args& a, int kernel, hipStream_t stream) {
+    if (!a.aligned) {
+        if (kernel == kI4Tile64) return many_launch<2, 1, 1, 1, 4, S, ZERO, GATED, true>(a, stream);
+        return many_launch<2, 2, 2, 2, 1, S, ZERO, GATED, true>(a, stream);
+    }
+    switch (kernel) {
+        case kI4Tile32: return many_launch<GATED ? 2 : 1, 1, 1, 1, 8, S, ZERO, GATED, false>(a, stream);
+        case kI4Tile64: return many_launch<2, 1, 1, 1, 4, S, ZERO, GATED, false>(a, stream);
+        case kI4Tile128: return many_launch<2, 2, 2, 1, 2, S, ZERO, GATED, false>(a, stream);
+        default: return many_launch<2, 4, 4, 1, 1, S, ZERO, GATED, false>(a, stream);
+    }
 }
 template <int S, bool GATED>
-lordba_status many(const I4Args& a, hipStream_t stream) {
-    return a.zero ? many<S, true, GATED>(a, stream) : many<S, false, GATED>(a, stream);
+lordba_status many(const I4Args& a, int kernel, hipStream_t stream) {
+    return a.zero ? many<S, true, GATED>(a, kernel, stream) : many<S, false, GATED>(a, kernel, stream);
 }
 template <bool GATED>
-lordba_status many(const I4Args& a, int64_t group, hipStream_t stream) {
-    return group == 32 ? many<4, GATED>(a, stream) : group == 64 ? many<2, GATED>(a, stream) : many<1, GATED>(a, stream);
+lordba_status many(const I4Args& a, int kernel, int64_t group, hipStream_t stream) {
+    return group == 32 ? many<4, GATED>(a, kernel, stream) : group == 64 ? many<2, GATED>(a, kernel, stream) : many<1, GATED>(a, kernel, stream);
 }
 
 }  // namespace
 
-lordba_status lordba_i4_many(const I4Args& a, int64_t group, bool gated, bool backward, hipStream_t stream) {
-    if (backward) return many<0, false>(a, stream);
-    return gated ? many<true>(a, group, stream) : many<false>(a, group, stream);
+lordba_status lordba_i4_many(const I4Args& a, int kernel, int64_t group, bool gated, bool backward, hipStream_t stream) {
+    if (backward) return many<0, false>(a, kernel, stream);
+    return gated ? many<true>(a, kernel, group, stream) : many<false>(a, kernel, group, stream);
 }

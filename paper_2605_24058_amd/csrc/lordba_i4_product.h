@@ -5,6 +5,7 @@
 #pragma once
 #include "lordba_dev_util.h"
 #include "lordba_i4.h"
+#include "lordba_i4_choice.h"
 #include "lordba_results.h"
 
 struct I4Args {
@@ -19,6 +20,8 @@ struct I4Args {
     int32_t tiles;             // blocks of 16 rows of a half
     int32_t groups;            // forward: along a row, padding included
     int32_t shift;             // backward: log2 of the group
+    int32_t columns;           // few tokens: that LDS holds at a time
+    int32_t aligned;           // whether rows of x consist of aligned 16-byte pieces
     uint32_t first;            // tile of this launch's first workgroup
 };
 
@@ -39,11 +42,17 @@ struct Zero8 {
     __device__ __forceinline__ h2 low_of(int p) const { return as_h2(z[p]); }
     __device__ __forceinline__ h2 high_of(int p) const { return h2{static_cast<_Float16>(960), static_cast<_Float16>(960)} - as_h2(z[p]); }
 };
+// The exponent's bits in a vector register: with the mask in a scalar one, "and" and "or" are one instruction (constants in the instruction itself make two).
+__device__ __forceinline__ uint32_t exponent() {
+    uint32_t v = 0x64006400u;
+    asm("" : "+v"(v));
+    return v;
+}
 template <class Z>
-__device__ __forceinline__ h8 operand(uint32_t w, const Z& z) {
+__device__ __forceinline__ h8 operand(uint32_t w, const Z& z, uint32_t exp) {
     const h2 sixteenth = {static_cast<_Float16>(0.0625f), static_cast<_Float16>(0.0625f)};
-    auto low = [&](uint32_t v, int p) { return as_h2((v & 0x000F000Fu) | 0x64006400u) - z.low_of(p); };
-    auto high = [&](uint32_t v, int p) { return __builtin_elementwise_fma(as_h2((v & 0x00F000F0u) | 0x64006400u), sixteenth, z.high_of(p)); };
+    auto low = [&](uint32_t v, int p) { return as_h2((v & 0x000F000Fu) | exp) - z.low_of(p); };
+    auto high = [&](uint32_t v, int p) { return __builtin_elementwise_fma(as_h2((v & 0x00F000F0u) | exp), sixteenth, z.high_of(p)); };
     const h2 a = low(w, 0), b = high(w, 1), c = low(w >> 8, 2), d = high(w >> 8, 3);
     return h8{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
 }
@@ -59,4 +68,4 @@ __device__ __forceinline__ float silu(float v) { return v * __builtin_amdgcn_rcp
 
 // The launches; arguments have been checked.
 lordba_status lordba_i4_few(const I4Args& a, int64_t group, bool gated, bool backward, hipStream_t stream);
-lordba_status lordba_i4_many(const I4Args& a, int64_t group, bool gated, bool backward, hipStream_t stream);
+lordba_status lordba_i4_many(const I4Args& a, int kernel, int64_t group, bool gated, bool backward, hipStream_t stream);

@@ -35,20 +35,20 @@ __device__ __forceinline__ void store8(_Float16* row, int64_t c, int64_t n, cons
             if (c + e < n) reinterpret_cast<uint16_t*>(row)[c + e] = static_cast<uint16_t>(v[e >> 1] >> (16 * (e & 1)));
     }
 }
-// The same for rows of which every other one starts in the middle of a word (an odd n), all lanes here: the four lane groups' 32 columns are stored
-// from their second column on, one further for each lane, so that the wide stores start on words (the memory path takes stores that do not apart).
+// The same for rows of which every other one starts in the middle of a word (an odd n), all lanes here: the 64 / LANES lane groups' columns, 32 of four, are
+// stored from their second column on, one further for each lane, so that the wide stores start on words (the memory path takes stores that do not apart).
 // 4096 x 8191 results 48 us -> 39 with 128 x 128 tiles, 50 -> 45 with 256 x 256.
-template <bool KEPT>
+template <bool KEPT, int LANES = 16>
 __device__ __forceinline__ void store8_odd(_Float16* p, const float (&f)[8]) {
     typedef uint32_t u3_word __attribute__((ext_vector_type(3), aligned(4)));
     const u4 v = to_halves<KEPT>(f);
-    const int g = (threadIdx.x & 63) >> 4;
+    const int g = (threadIdx.x & 63) / LANES;
     const bool odd = (reinterpret_cast<uintptr_t>(p) & 2) != 0;
-    const uint32_t next = static_cast<uint32_t>(__shfl_down(static_cast<int>(v[0]), 16));
+    const uint32_t next = static_cast<uint32_t>(__shfl_down(static_cast<int>(v[0]), LANES));
     const u4 moved = {__builtin_amdgcn_alignbit(v[1], v[0], 16), __builtin_amdgcn_alignbit(v[2], v[1], 16), __builtin_amdgcn_alignbit(v[3], v[2], 16),
                       __builtin_amdgcn_alignbit(next, v[3], 16)};
     uint16_t* const h = reinterpret_cast<uint16_t*>(p);
-    if (!odd || g < 3) {
+    if (!odd || g < 64 / LANES - 1) {
         u4_word* const to = reinterpret_cast<u4_word*>(h + odd);
         *to = odd ? moved : v;
     } else {

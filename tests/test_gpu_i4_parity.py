@@ -28,28 +28,19 @@ def laid_out(torch, mem, codes, scale, zero, group, halves=1, transposed=False):
     return out
 
 
-# T, d_in, d_out, group, zero points: one token and one column; ends of groups, of blocks of 128 columns, of 32 rows; both sides of the kernels' limits; odd
-# widths; rows that start anywhere; tiles of either size with all sizes ragged
-SHAPES = [(1, 1, 1, 32, True), (1, 128, 32, 128, False), (2, 31, 33, 32, True), (3, 127, 31, 64, False), (15, 129, 65, 128, True), (16, 256, 64, 64, True),
-          (17, 257, 95, 32, False), (33, 640, 96, 128, False), (40, 1000, 130, 64, True), (64, 384, 100, 32, True), (64, 2176, 48, 128, True),
-          (65, 384, 96, 128, False), (65, 129, 127, 32, True), (127, 1000, 257, 64, True), (128, 256, 128, 128, False), (200, 100, 300, 32, False),
-          (333, 392, 1031, 64, False), (513, 130, 515, 128, True), (1030, 264, 4104, 32, True), (2200, 384, 2049, 64, False), (2048, 128, 6144, 128, True),
-          (100, 5, 700, 32, True), (70, 7, 3, 64, False), (5, 4, 9, 32, False)]
-
-
 def acts(torch, rng, rows, cols):
     return torch.from_numpy(i8_checks.acts(rng, rows, cols)).cuda()
 
 
 @pytest.mark.parametrize("shift", [0, 1], ids=["aligned", "by-one"])
-@pytest.mark.parametrize("T,d_in,d_out,group,zeros", SHAPES)
+@pytest.mark.parametrize("T,d_in,d_out,group,zeros", i4_checks.SHAPES)
 def test_linear_and_gradient(torch, T, d_in, d_out, group, zeros, shift):
     rng = np.random.default_rng(T + d_in)
     mem = i8_checks.Memory(torch)
     codes, scale, zero = i4_checks.weights(torch, rng, d_out, d_in, group, zeros)
     x, g = mem.input(acts(torch, rng, T, d_in), shift), mem.input(acts(torch, rng, T, d_out), shift)
     for backward in (False, True):
-        W = i4_checks.real(torch, codes, scale, zero, group, rounded=backward or T > i4_checks.FEW).cuda()
+        W = i4_checks.real(torch, codes, scale, zero, group, rounded=backward or i4_checks.kernel(T, d_in, d_out, aligned=shift == 0) != "few").cuda()
         y = mem.output((T, d_in if backward else d_out), torch.float16, shift)
         i8_checks.call(torch, "lordba_linear_i4" + "_backward" * backward, g if backward else x, *laid_out(torch, mem, codes, scale, zero, group, 1, backward), y,
                        T, d_in, d_out, group)
@@ -59,13 +50,13 @@ def test_linear_and_gradient(torch, T, d_in, d_out, group, zeros, shift):
 
 
 @pytest.mark.parametrize("shift", [0, 1], ids=["aligned", "by-one"])
-@pytest.mark.parametrize("T,d_in,d_ff,group,zeros", [s for s in SHAPES if s[1] * s[2] < 600000])
+@pytest.mark.parametrize("T,d_in,d_ff,group,zeros", i4_checks.SHAPES)
 def test_gated_and_gradient(torch, T, d_in, d_ff, group, zeros, shift):
     rng = np.random.default_rng(T + d_in + 1)
     mem = i8_checks.Memory(torch)
     codes, scale, zero = i4_checks.weights(torch, rng, 2 * d_ff, d_in, group, zeros)
     x, add, dh = mem.input(acts(torch, rng, T, d_in), shift), mem.input(torch.randn(2, T, d_ff).half().cuda(), shift), mem.input(acts(torch, rng, T, d_ff), shift)
-    W = i4_checks.real(torch, codes, scale, zero, group, rounded=T > i4_checks.FEW).cuda()
+    W = i4_checks.real(torch, codes, scale, zero, group, rounded=i4_checks.kernel(T, d_in, d_ff, gated=True, aligned=shift == 0) != "few").cuda()
     L = laid_out(torch, mem, codes, scale, zero, group, 2)
     both, err = i4_checks.product(torch, x.double(), W)
     for addends, keep in ((add, True), (None, False)):
