@@ -21,7 +21,9 @@ constexpr I4Tile kI4Tiles[5] = {{32, 16, 8, 2, 1.6, 1.7, 3.0},     // kernel for
                                 {64, 32, 4, 2, 1.1, 1.05, 2.5},
                                 {128, 64, 2, 2, 1.15, 1.2, 2.5},
                                 {256, 128, 1, 2, 1.3, 1.9, 3.0}};
-constexpr I4Tile kI4Unaligned[2] = {{64, 32, 4, 2, 2.0, 2.0, 2.5}, {128, 128, 1, 2, 2.0, 2.2, 3.0}};   // kI4Tile64 and kI4Tile128 for rows that no request takes whole
+// The same for rows that no request takes whole, which come through registers.  (The second waits longer than the third: nothing chooses it.)
+constexpr I4Tile kI4Unaligned[5] = {{32, 16, 8, 2, 2.0, 2.0, 3.0}, {32, 32, 8, 1, 3.4, 3.4, 3.0}, {64, 32, 4, 2, 1.8, 1.3, 2.5}, {128, 64, 2, 2, 1.75, 1.57, 2.5},
+                                    {256, 128, 1, 2, 1.8, 2.5, 3.0}};
 
 constexpr int64_t kI4MostColumns = 1 << 22;   // of a plane: a tile's rows span less than 4 GiB
 constexpr int64_t kI4FewTokens = 8;           // up to here a tile's other tokens would be none
@@ -37,10 +39,10 @@ inline I4Kernel i4_kernel(int64_t T, int64_t k, int64_t blocks, int64_t n, bool 
     if (T <= kI4FewTokens || k < 8 || k > kI4MostColumns) return kI4Few;
     const int64_t channels = gated ? 2 * n : n;
     I4Kernel best = kI4Few;
-    double least = i4_cost(kI4Tiles[0], channels, T, blocks);
+    double least = i4_cost((aligned ? kI4Tiles : kI4Unaligned)[0], channels, T, blocks);
     for (int i = 1; i < 5; ++i) {
-        if (!aligned && i != kI4Tile64 && i != kI4Tile128) continue;
-        I4Tile t = aligned ? kI4Tiles[i] : kI4Unaligned[i - kI4Tile64];
+        if (!aligned && i == kI4Tile32) continue;
+        I4Tile t = (aligned ? kI4Tiles : kI4Unaligned)[i];
         if (gated && i == kI4Tile32) t.channels = 64, t.share *= 1.3;
         const double cost = i4_cost(t, channels, T, blocks);
         if (cost < least) best = static_cast<I4Kernel>(i), least = cost;

@@ -106,47 +106,52 @@ __global__ __launch_bounds__(64 * NW, NW == 8 ? 4 : 1) void lordba_i4_few_kernel
 #pragma unroll
         for (int j = 0; j < D; ++j) load(at(j), ring[j]);
         if (b0 > 0) __syncthreads();   // (everybody has read what lies there)
-        // The activations: 256 bytes of a row a time, 16 to a lane, four of those a wave.  What is behind the rows' end is 0.
-        auto place = [&](int k, int& t, int& plane, int64_t& c) __attribute__((always_inline)) {   // unit k of the workgroup's, this lane's piece
-            t = k / there;
-            const int in = b0 + min(k % there, blocks - 1);
-            plane = in >= a.plane_blocks ? 1 : 0;
-            c = static_cast<int64_t>(in - plane * a.plane_blocks) * kI4Columns + 8 * ((lane & 15) ^ t);
+        // The activations: 256 bytes of a row a time, 16 to a lane, four of those a wave.  What is behind the rows' end is 0.  (All in 32 bits, the division
+        // by a product that is exact for the few thousand units there are: with 64-bit steps and a division it took 3 us where the rest takes 5.)
+        const int units = tokens * there, columns = static_cast<int>(a.k), last = max(columns - 8, 0);
+        const float by = __builtin_amdgcn_rcpf(static_cast<float>(there));
+        auto place = [&](int k, const _Float16*& x, int& c) __attribute__((always_inline)) {   // unit k of the workgroup's, this lane's piece: its row, its column
+            const int t = static_cast<int>((static_cast<float>(k) + 0.5f) * by), in = b0 + min(k - t * there, blocks - 1);
+            const bool second = in >= a.plane_blocks;
+            c = (second ? in - a.plane_blocks : in) * static_cast<int>(kI4Columns) + 8 * ((lane & 15) ^ t);
+            x = a.x + (t0 + (second ? a.T : 0)) * a.k + static_cast<uint32_t>(t * columns);
         };
-        const int units = tokens * there;
         if (a.aligned) {
             for (int k0 = 4 * wave; k0 < units; k0 += 4 * NW) {
-                int t, plane;
-                int64_t c;
-                place(min(k0 + q, units - 1), t, plane, c);
-                load16_to_lds<false>(base + k0 * 256u, a.x + (plane * a.T + t0 + t) * a.k + min(c, a.k - 8));
+                const _Float16* x;
+                int c;
+                place(min(k0 + q, units - 1), x, c);
+                load16_to_lds<false>(base + k0 * 256u, x + min(c, last));
             }
             asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-            for (int k0 = 4 * wave; a.k % kI4Columns != 0 && k0 + q < units; k0 += 4 * NW) {
-                int t, plane;
-                int64_t c;
-                place(k0 + q, t, plane, c);
-                if (c >= a.k) *reinterpret_cast<u4*>(lds + (k0 + q) * 256 + 16 * (lane & 15)) = u4{0u, 0u, 0u, 0u};
+            for (int k0 = 4 * wave; columns % kI4Columns != 0 && k0 + q < units; k0 += 4 * NW) {
+                const _Float16* x;
+                int c;
+                place(k0 + q, x, c);
+                if (c >= columns) *reinterpret_cast<u4*>(lds + (k0 + q) * 256 + 16 * (lane & 15)) = u4{0u, 0u, 0u, 0u};
             }
         } else {
-            constexpr int U = 4;
+            constexpr int U = 4;   // requested together
             for (int k0 = 4 * wave; k0 < units; k0 += 4 * NW * U) {
                 u4 v[U];
-                int over[U];
 #pragma unroll
                 for (int u = 0; u < U; ++u) {
-                    int t, plane;
-                    int64_t c;
-                    place(min(k0 + 4 * NW * u + q, units - 1), t, plane, c);
-                    const _Float16* const row = a.x + (plane * a.T + t0 + t) * a.k;
-                    over[u] = static_cast<int>(min<int64_t>(c - max<int64_t>(a.k - 8, 0), 8));
-                    if (a.k >= 8) v[u] = load16_any(row + min(c, a.k - 8));
-                    else v[u] = load_part(row, 0, a.k);
+                    if (k0 + 4 * NW * u >= units) break;
+                    const _Float16* x;
+                    int c;
+                    place(min(k0 + 4 * NW * u + q, units - 1), x, c);
+                    if (columns >= 8) v[u] = load16_any(x + min(c, last));
+                    else v[u] = load_part(x, 0, columns);
                 }
 #pragma unroll
-                for (int u = 0; u < U; ++u)
-                    if (k0 + 4 * NW * u + q < units)
-                        *reinterpret_cast<u4*>(lds + (k0 + 4 * NW * u + q) * 256 + 16 * (lane & 15)) = over[u] > 0 ? drop_halves(v[u], over[u]) : v[u];
+                for (int u = 0; u < U; ++u) {
+                    const int k = k0 + 4 * NW * u + q;
+                    if (k >= units) break;
+                    const _Float16* x;
+                    int c;
+                    place(k, x, c);
+                    *reinterpret_cast<u4*>(lds + k * 256 + 16 * (lane & 15)) = c > last ? drop_halves(v[u], min(c - last, 8)) : v[u];
+                }
             }
         }
         __syncthreads();

@@ -87,7 +87,10 @@ __global__ __launch_bounds__(64 * WC * WT * WK, 2) void lordba_i4_many_kernel(I4
     static_assert(kTokens / 4 % NW == 0, "whole loads per wave");
     const int32_t last_row = static_cast<int32_t>(min<int64_t>(a.T - 1 - first_token, kTokens - 1));
     const int32_t row0 = 4 * wi + (lane >> 4);
-    u4 held[BY_REGISTERS ? kLoads : 1];
+    // (a large tile's accumulators leave room for half of a step's activations: those of the next step are requested and stored half by half then)
+    constexpr bool HALVES = BY_REGISTERS && CP * TB >= 8;
+    constexpr int kHeld = HALVES ? kLoads / 2 : kLoads;
+    u4 held[BY_REGISTERS ? kHeld : 1];
     // (of the WK blocks of a step this wave has the wk-th; where there is none, the last stands in, behind the rows' end altogether)
     auto block_of = [&](int step) __attribute__((always_inline)) { return min(step * WK + wk, a.blocks - 1); };
     auto column_of = [&](int b) __attribute__((always_inline)) { return (b >= a.plane_blocks ? b - a.plane_blocks : b) * static_cast<int32_t>(kI4Columns); };
@@ -102,7 +105,7 @@ __global__ __launch_bounds__(64 * WC * WT * WK, 2) void lordba_i4_many_kernel(I4
         const _Float16* const x = a.x + ((b >= a.plane_blocks ? a.T : 0) + first_token) * a.k;
         // (a tile's rows span less than 4 GiB: what the launch sees to)
         const uint32_t at = (static_cast<uint32_t>(min(row0 + 4 * NW * i, last_row)) * static_cast<uint32_t>(k) + min(c0 + piece_of(i), k - 8)) * 2u;
-        if constexpr (BY_REGISTERS) held[i] = load16_any(reinterpret_cast<const char*>(x) + at);
+        if constexpr (BY_REGISTERS) held[i % kHeld] = load16_any(reinterpret_cast<const char*>(x) + at);
         else load16_to_lds_from(base + buffer + (wi + NW * i) * 1024u, x, at);
     };
     auto request_scales = [&](int step, uint32_t buffer) __attribute__((always_inline)) {
@@ -117,21 +120,21 @@ __global__ __launch_bounds__(64 * WC * WT * WK, 2) void lordba_i4_many_kernel(I4
             }
         }
     };
-    auto stage = [&](int step, uint32_t buffer) __attribute__((always_inline)) {
-#pragma unroll
-        for (int i = 0; i < kLoads; ++i) request(step, buffer, i);
-        request_scales(step, buffer);
-    };
-    auto store_held = [&](int step, uint32_t buffer) __attribute__((always_inline)) {
+    auto store_held = [&](int step, uint32_t buffer, int first) __attribute__((always_inline)) {
         if constexpr (BY_REGISTERS) {
             const int32_t end = end_of(step, wk);
 #pragma unroll
-            for (int i = 0; i < kLoads; ++i) {
+            for (int l = 0; l < kHeld; ++l) {
+                const int i = first + l;
                 const int32_t over = piece_of(i) - (end - 8);
-                if (end < kI4Columns && over > 0) held[i] = drop_halves(held[i], over);
-                *reinterpret_cast<u4*>(lds + buffer + (wi + NW * i) * 1024u + 16 * lane) = held[i];
+                if (end < kI4Columns && over > 0) held[l] = drop_halves(held[l], over);
+                *reinterpret_cast<u4*>(lds + buffer + (wi + NW * i) * 1024u + 16 * lane) = held[l];
             }
         }
+    };
+    auto request_some = [&](int step, uint32_t buffer, int first, int n) __attribute__((always_inline)) {
+#pragma unroll
+        for (int l = 0; l < n; ++l) request(step, buffer, first + l);
     };
     // Pieces of a step behind the rows' end, when everything has landed; whoever requested a piece clears it.
     auto clear_end = [&](int step, uint32_t buffer) __attribute__((always_inline)) {
@@ -213,35 +216,50 @@ __global__ __launch_bounds__(64 * WC * WT * WK, 2) void lordba_i4_many_kernel(I4
             }
         }
     };
+    using std::integral_constant;
     Weights now, next;
-    stage(0, 0);
+    request_scales(0, 0);
     load_weights(block_of(0), now);
-    store_held(0, 0);
+    if constexpr (HALVES) {
+        request_some(0, 0, 0, kHeld);
+        store_held(0, 0, 0);
+        request_some(0, 0, kHeld, kHeld);
+        store_held(0, 0, kHeld);
+    } else {
+        request_some(0, 0, 0, kLoads);
+        store_held(0, 0, 0);
+    }
     meet();
     clear_end(0, 0);
-    stage(min(1, steps - 1), kBuffer);
+    request_scales(min(1, steps - 1), kBuffer);
+    if constexpr (!HALVES) request_some(min(1, steps - 1), kBuffer, 0, kLoads);
     load_weights(block_of(min(1, steps - 1)), next);
-    operands(std::integral_constant<int, 0>{}, 0, now);
+    operands(integral_constant<int, 0>{}, 0, now);
     uint32_t buffer = 0;
     for (int step = 0; step < steps; ++step) {
+        // (Behind the last step what is there is requested once more, operands are made of it, and nobody multiplies them.)
+        const int next_step = min(step + 1, steps - 1), behind = min(step + 2, steps - 1);
         auto depth = [&](auto d) __attribute__((always_inline)) {
-            operands(std::integral_constant<int, d.value + 1>{}, buffer, now);
-            multiply(std::integral_constant<int, d.value & 1>{});
+            operands(integral_constant<int, d.value + 1>{}, buffer, now);
+            multiply(integral_constant<int, d.value & 1>{});
             weave();
         };
-        depth(std::integral_constant<int, 0>{});
-        depth(std::integral_constant<int, 1>{});
-        depth(std::integral_constant<int, 2>{});
-        depth(std::integral_constant<int, 3>{});
-        depth(std::integral_constant<int, 4>{});
-        depth(std::integral_constant<int, 5>{});
-        depth(std::integral_constant<int, 6>{});
+        if constexpr (HALVES) request_some(next_step, 0, 0, kHeld);
+        depth(integral_constant<int, 0>{});
+        depth(integral_constant<int, 1>{});
+        depth(integral_constant<int, 2>{});
+        if constexpr (HALVES) {
+            store_held(next_step, kBuffer - buffer, 0);
+            request_some(next_step, 0, kHeld, kHeld);
+        }
+        depth(integral_constant<int, 3>{});
+        depth(integral_constant<int, 4>{});
+        depth(integral_constant<int, 5>{});
+        depth(integral_constant<int, 6>{});
         // (the operands of depth 7 are made above, not behind the barrier)
 #pragma unroll
         for (int i = 0; i < CP; ++i) asm volatile("" : "+v"(w[1][i]));
-        // (Behind the last step what is there is requested once more, operands are made of it, and nobody multiplies them.)
-        const int next_step = min(step + 1, steps - 1), behind = min(step + 2, steps - 1);
-        store_held(next_step, kBuffer - buffer);
+        store_held(next_step, kBuffer - buffer, kLoads - kHeld);
         meet();
         clear_end(next_step, kBuffer - buffer);
         now = next;
@@ -250,10 +268,9 @@ __global__ __launch_bounds__(64 * WC * WT * WK, 2) void lordba_i4_many_kernel(I4
         request_scales(behind, buffer);
         const uint32_t freed = buffer;
         buffer = kBuffer - buffer;
-        operands(std::integral_constant<int, 0>{}, buffer, now);
-#pragma unroll
-        for (int l = 0; l < kLoads; ++l) request(behind, freed, l);
-        multiply(std::integral_constant<int, 1>{});
+        operands(integral_constant<int, 0>{}, buffer, now);
+        if constexpr (!HALVES) request_some(behind, freed, 0, kLoads);
+        multiply(integral_constant<int, 1>{});
         weave();
     }
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // (nothing is on its way into LDS when the workgroup ends, or takes it for its sums)
@@ -380,7 +397,8 @@ template <int S, bool ZERO, bool GATED>
 lordba_status many(const I4Args& a, int kernel, hipStream_t stream) {
     if (!a.aligned) {
         if (kernel == kI4Tile64) return many_launch<2, 1, 1, 1, 4, S, ZERO, GATED, true>(a, stream);
-        return many_launch<2, 2, 2, 2, 1, S, ZERO, GATED, true>(a, stream);
+        if (kernel == kI4Tile128) return many_launch<2, 2, 2, 1, 2, S, ZERO, GATED, true>(a, stream);
+        return many_launch<2, 4, 4, 1, 1, S, ZERO, GATED, true>(a, stream);
     }
     switch (kernel) {
         case kI4Tile32: return many_launch<GATED ? 2 : 1, 1, 1, 1, 8, S, ZERO, GATED, false>(a, stream);
