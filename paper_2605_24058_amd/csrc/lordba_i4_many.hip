@@ -157,21 +157,36 @@ __global__ __launch_bounds__(64 * WC * WT * WK, 2) void lordba_i4_many_kernel(I4
         for (int j = 0; j < TB; ++j)
 #pragma unroll
             for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.f;
-    // operands of depth d = 2 m + c of a step
+    // Operands of depth d = 2 m + c of a step: the activations are read A - 1 depths ahead (a small tile's products of one depth do not last as long as a
+    // read of LDS takes), the weights are made from the codes one depth ahead.
+    constexpr int A = CP * TB >= 8 ? 2 : CP * TB >= 4 || BWD ? 4 : 8;
     const int8_t* const mine = lds + (wt * TB * 32 + n) * 256;
-    h8 x[2][TB], w[2][CP];
+    h8 x[A][TB], w[2][CP];
+    u4 sv[BWD && A > 2 ? A : 1][CP], zv[BWD && A > 2 && ZERO ? A : 1][CP];
     const uint32_t exp = exponent();
-    auto operands = [&](auto depth, uint32_t buffer, const Weights& v) __attribute__((always_inline)) {
-        constexpr int d = depth.value, m = d >> 1, c = d & 1, set = d & 1;
+    auto read = [&](auto depth, uint32_t buffer) __attribute__((always_inline)) {
+        constexpr int d = depth.value, set = d % A;
 #pragma unroll
         for (int j = 0; j < TB; ++j) x[set][j] = as_h8(*reinterpret_cast<const u4*>(mine + buffer + j * 8192 + 16 * ((2 * d + h) ^ (n & 15))));
+        if constexpr (BWD && A > 2) {
+#pragma unroll
+            for (int i = 0; i < CP; ++i) {
+                const int8_t* const s = lds + buffer + kX + s_at[i] + 32 * d + 16 * h;
+                sv[set][i] = *reinterpret_cast<const u4*>(s);
+                if constexpr (ZERO) zv[set][i] = *reinterpret_cast<const u4*>(s + kS);
+            }
+        }
+    };
+    auto make = [&](auto depth, uint32_t buffer, const Weights& v) __attribute__((always_inline)) {
+        constexpr int d = depth.value, m = d >> 1, c = d & 1, set = d & 1;
 #pragma unroll
         for (int i = 0; i < CP; ++i) {
             if constexpr (BWD) {
-                const int8_t* const s = lds + buffer + kX + s_at[i] + 32 * d + 16 * h;
-                if constexpr (ZERO) w[set][i] = operand(v.c[i][c][m], Zero8{*reinterpret_cast<const u4*>(s + kS)}, exp);
+                const int8_t* const at_s = lds + buffer + kX + s_at[i] + 32 * d + 16 * h;
+                const u4 s = A > 2 ? sv[d % A][i] : *reinterpret_cast<const u4*>(at_s);
+                if constexpr (ZERO) w[set][i] = operand(v.c[i][c][m], Zero8{A > 2 ? zv[d % A][i] : *reinterpret_cast<const u4*>(at_s + kS)}, exp);
                 else w[set][i] = operand(v.c[i][c][m], Zero1(kZero8), exp);
-                w[set][i] = w[set][i] * as_h8(*reinterpret_cast<const u4*>(s));
+                w[set][i] = w[set][i] * as_h8(s);
             } else {
                 constexpr int g = m * (S ? S : 1) / 4;
                 w[set][i] = operand(v.c[i][c][m], Zero1(ZERO ? v.z[i][g] : kZero8), exp);
@@ -180,11 +195,12 @@ __global__ __launch_bounds__(64 * WC * WT * WK, 2) void lordba_i4_many_kernel(I4
             }
         }
     };
-    auto multiply = [&](auto set) __attribute__((always_inline)) {
+    auto multiply = [&](auto depth) __attribute__((always_inline)) {
+        constexpr int d = depth.value;
 #pragma unroll
         for (int i = 0; i < CP; ++i)
 #pragma unroll
-            for (int j = 0; j < TB; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(w[set.value][i], x[set.value][j], acc[i][j], 0, 0, 0);
+            for (int j = 0; j < TB; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(w[d & 1][i], x[d % A][j], acc[i][j], 0, 0, 0);
     };
     // between every few products some of the next operands' work
     auto weave = []() __attribute__((always_inline)) {
@@ -234,14 +250,29 @@ __global__ __launch_bounds__(64 * WC * WT * WK, 2) void lordba_i4_many_kernel(I4
     request_scales(min(1, steps - 1), kBuffer);
     if constexpr (!HALVES) request_some(min(1, steps - 1), kBuffer, 0, kLoads);
     load_weights(block_of(min(1, steps - 1)), next);
-    operands(integral_constant<int, 0>{}, 0, now);
+    auto read_first = [&](uint32_t buffer) __attribute__((always_inline)) {   // what depth 0 expects to be there
+        read(integral_constant<int, 0>{}, buffer);
+        if constexpr (A > 2) {
+            read(integral_constant<int, 1>{}, buffer);
+            read(integral_constant<int, 2>{}, buffer);
+        }
+        if constexpr (A > 4) {
+            read(integral_constant<int, 3>{}, buffer);
+            read(integral_constant<int, 4>{}, buffer);
+            read(integral_constant<int, 5>{}, buffer);
+            read(integral_constant<int, 6>{}, buffer);
+        }
+    };
+    read_first(0);
+    make(integral_constant<int, 0>{}, 0, now);
     uint32_t buffer = 0;
     for (int step = 0; step < steps; ++step) {
         // (Behind the last step what is there is requested once more, operands are made of it, and nobody multiplies them.)
         const int next_step = min(step + 1, steps - 1), behind = min(step + 2, steps - 1);
         auto depth = [&](auto d) __attribute__((always_inline)) {
-            operands(integral_constant<int, d.value + 1>{}, buffer, now);
-            multiply(integral_constant<int, d.value & 1>{});
+            if constexpr (d.value + A - 1 < 8) read(integral_constant<int, d.value + A - 1>{}, buffer);
+            make(integral_constant<int, d.value + 1>{}, buffer, now);
+            multiply(d);
             weave();
         };
         if constexpr (HALVES) request_some(next_step, 0, 0, kHeld);
@@ -268,9 +299,10 @@ __global__ __launch_bounds__(64 * WC * WT * WK, 2) void lordba_i4_many_kernel(I4
         request_scales(behind, buffer);
         const uint32_t freed = buffer;
         buffer = kBuffer - buffer;
-        operands(integral_constant<int, 0>{}, buffer, now);
+        read_first(buffer);
+        make(integral_constant<int, 0>{}, buffer, now);
         if constexpr (!HALVES) request_some(behind, freed, 0, kLoads);
-        multiply(integral_constant<int, 1>{});
+        multiply(integral_constant<int, 7>{});
         weave();
     }
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // (nothing is on its way into LDS when the workgroup ends, or takes it for its sums)
@@ -396,6 +428,7 @@ lordba_status many_launch(I4Args a, hipStream_t stream) {
 template <int S, bool ZERO, bool GATED>
 lordba_status many(const I4Args& a, int kernel, hipStream_t stream) {
     if (!a.aligned) {
+        if (kernel == kI4Tile32) return many_launch<GATED ? 2 : 1, 1, 1, 1, 8, S, ZERO, GATED, true>(a, stream);
         if (kernel == kI4Tile64) return many_launch<2, 1, 1, 1, 4, S, ZERO, GATED, true>(a, stream);
         if (kernel == kI4Tile128) return many_launch<2, 2, 2, 1, 2, S, ZERO, GATED, true>(a, stream);
         return many_launch<2, 4, 4, 1, 1, S, ZERO, GATED, true>(a, stream);

@@ -22,7 +22,7 @@ def test_every_kernel_is_reached():
     for form in ("linear", "gradient", "gated", "gated gradient"):
         for kernel in i4_checks.KERNELS:
             assert (form, kernel, True) in reached, (form, kernel)
-        for kernel in ("few", "tile64", "tile128", "tile256"):
+        for kernel in i4_checks.KERNELS:
             assert (form, kernel, False) in reached, (form, kernel)
         # both answers of each question somewhere among a form's kernels, every group
         both = set().union(*(r for (f, _, _), r in reached.items() if f == form))
@@ -36,5 +36,3 @@ def test_limits():
     assert k(4096, 7, 4096) == k(100, (1 << 22) + 8, 64) == "few"                 # what the tiles do not take
     assert k(4096, 11008, 4096) == k(2048, 4096, 11008, gated=True) == "tile256"
     assert k(4096, 4096, 4096, aligned=False) == "tile256"
-    for T in (9, 40, 300, 5000):
-        assert k(T, 1001, 999) != "tile32"
