@@ -1,9 +1,10 @@
-"""A feed-forward block (gate, up, down) whose frozen weights are held in 8 bits and whose three projections carry LoRDBA adapters:
+"""A feed-forward block (gate, up, down) whose frozen weights are held in 8 or in 4 bits and whose three projections carry LoRDBA adapters:
 the library's calls in the order in which a training loop and a serving loop make them.
 
-    python -m paper_2605_24058_amd.adapted_block [--tokens 512] [--d-model 1024] [--d-ff 2752] [--rank 16] [--steps 20]
+    python -m paper_2605_24058_amd.adapted_block [--tokens 512] [--d-model 1024] [--d-ff 2752] [--rank 16] [--steps 20] [--bits 4] [--vocab 8192 [--top 16]]
 
-fits the adapters to what the same block answers with stronger branches, prints the loss, then answers as a decode step would.
+fits the adapters to what the same block answers with stronger branches, prints the loss, then answers as a decode step would.  With --vocab the
+answers go through a frozen head on 4-bit weights, and what the adapters learn from are the stronger block's top logits.
 """
 from __future__ import annotations
 
@@ -41,20 +42,50 @@ class Adapter:
         self.pack()
 
 
+def frozen_in_4_bits(w, group: int = 128, halves: int = 1):
+    """fp16 weights as the 4-bit projections take them, and as their input gradients do."""
+    plain = lb.lordba_quantize_i4(w, group, zero_points=True)
+    return tuple(lb.lordba_layout_i4(*plain, group, halves=halves, transposed=t) for t in (False, True))
+
+
 class AdaptedBlock:
     """y = down(silu(gate(x)) * up(x)), each projection its frozen 8-bit part plus its adapter's branch."""
 
-    def __init__(self, d_model: int, d_ff: int, r: int, p: float = 0.05, seed: int = 0):
+    def __init__(self, d_model: int, d_ff: int, r: int, p: float = 0.05, seed: int = 0, bits: int = 8):
         gen = torch.Generator(device="cuda").manual_seed(seed)
-        self.d_model, self.d_ff, self.p, self.seed = d_model, d_ff, p, seed
+        self.d_model, self.d_ff, self.p, self.seed, self.bits = d_model, d_ff, p, seed, bits
         # the frozen weights, laid out once; the transposed layouts are what the input gradients contract with
         half = lambda n, k: (torch.randn(n, k, generator=gen, device="cuda") / k ** 0.5).half()
-        self.gate_up, self.gate_up_scale = lb.lordba_quantize_rows(torch.cat([half(d_ff, d_model), half(d_ff, d_model)]))
-        self.down, self.down_scale = lb.lordba_quantize_rows(half(d_model, d_ff))
-        self.gate_up_t = lb.lordba_layout_i8(self.gate_up[:, :d_model].contiguous(), transposed=True)
-        self.down_t = lb.lordba_layout_i8(self.down[:, :d_ff].contiguous(), transposed=True)
+        gate_up, down = torch.cat([half(d_ff, d_model), half(d_ff, d_model)]), half(d_model, d_ff)
+        if bits == 4:
+            self.gate_up, self.gate_up_t = frozen_in_4_bits(gate_up, halves=2)
+            self.down, self.down_t = frozen_in_4_bits(down)
+        elif bits == 8:
+            self.gate_up, self.gate_up_scale = lb.lordba_quantize_rows(gate_up)
+            self.down, self.down_scale = lb.lordba_quantize_rows(down)
+            self.gate_up_t = lb.lordba_layout_i8(self.gate_up[:, :d_model].contiguous(), transposed=True)
+            self.down_t = lb.lordba_layout_i8(self.down[:, :d_ff].contiguous(), transposed=True)
+        else:
+            raise ValueError("bits must be 8 or 4")
         self.adapters = {name: Adapter(*shape, r, gen) for name, shape in
                          (("gate", (d_model, d_ff)), ("up", (d_model, d_ff)), ("down", (d_ff, d_model)))}
+
+    # the four products with the frozen weights
+    def _gated(self, x, addends, save=False):
+        if self.bits == 4:
+            return lb.lordba_gated_i4(x, self.gate_up, addends=addends, save=save)
+        return lb.lordba_gated_i8(x, self.gate_up, self.gate_up_scale, addends=addends, save=save)
+
+    def _gated_backward(self, dh, kept):
+        if self.bits == 4:
+            return lb.lordba_gated_i4_backward(dh, kept, self.gate_up_t)
+        return lb.lordba_gated_i8_backward(dh, kept, self.gate_up_t, self.gate_up_scale)
+
+    def _down(self, h):
+        return lb.lordba_linear_i4(h, self.down) if self.bits == 4 else lb.lordba_linear_i8(h, self.down, self.down_scale)
+
+    def _down_backward(self, dy):
+        return lb.lordba_linear_i4_backward(dy, self.down_t) if self.bits == 4 else lb.lordba_linear_i8_backward(dy, self.down_t, self.down_scale)
 
     def serve(self, x):
         """The block in inference: no dropout, nothing kept."""
@@ -63,9 +94,9 @@ class AdaptedBlock:
         for k, name in enumerate(("gate", "up")):
             a = self.adapters[name]
             lb.lordba_forward(x, *a.packed[:2], *a.half, zero[k], y_out=add[k])
-        h = lb.lordba_gated_i8(x, self.gate_up, self.gate_up_scale, addends=add)
+        h = self._gated(x, add)
         a = self.adapters["down"]
-        return lb.lordba_forward(h, *a.packed[:2], *a.half, lb.lordba_linear_i8(h, self.down, self.down_scale))
+        return lb.lordba_forward(h, *a.packed[:2], *a.half, self._down(h))
 
     def forward(self, x, step: int):
         """The block in training: the branches see their inputs through dropout.  Returns y and what the backward pass needs (no masks: they follow
@@ -73,9 +104,9 @@ class AdaptedBlock:
         xd = lb.lordba_dropout(x, self.p, self.seed, 2 * step)
         zero = x.new_zeros(x.shape[0], self.d_ff)
         (gate, t_gate), (up, t_up) = (self.adapters[n].branch(xd, zero) for n in ("gate", "up"))
-        h, kept = lb.lordba_gated_i8(x, self.gate_up, self.gate_up_scale, addends=torch.stack([gate, up]), save=True)
+        h, kept = self._gated(x, torch.stack([gate, up]), save=True)
         hd = lb.lordba_dropout(h, self.p, self.seed, 2 * step + 1)
-        y, t_down = self.adapters["down"].branch(hd, lb.lordba_linear_i8(h, self.down, self.down_scale))
+        y, t_down = self.adapters["down"].branch(hd, self._down(h))
         return y, (xd, hd, kept, t_gate, t_up, t_down, step)
 
     def backward(self, dy, saved, kappa: float = 100.0):
@@ -83,8 +114,8 @@ class AdaptedBlock:
         xd, hd, kept, t_gate, t_up, t_down, step = saved
         grads = {"down": self.adapters["down"].branch_backward(hd, dy, t_down, torch.zeros_like(hd), kappa)}
         # the branch's input gradient passes its mask again, and the base path's is added on the way
-        dh = lb.lordba_dropout(grads["down"]["dx"], self.p, self.seed, 2 * step + 1, y_base=lb.lordba_linear_i8_backward(dy, self.down_t, self.down_scale))
-        dx, dgate_up = lb.lordba_gated_i8_backward(dh, kept, self.gate_up_t, self.gate_up_scale)
+        dh = lb.lordba_dropout(grads["down"]["dx"], self.p, self.seed, 2 * step + 1, y_base=self._down_backward(dy))
+        dx, dgate_up = self._gated_backward(dh, kept)
         grads["gate"] = self.adapters["gate"].branch_backward(xd, dgate_up[0], t_gate, torch.zeros_like(xd), kappa)
         grads["up"] = self.adapters["up"].branch_backward(xd, dgate_up[1], t_up, grads["gate"]["dx"], kappa)     # (both branches have the same input)
         return lb.lordba_dropout(grads["up"]["dx"], self.p, self.seed, 2 * step, y_base=dx), grads
@@ -103,6 +134,47 @@ def fit(block: AdaptedBlock, x, target, steps: int, rate: float = 0.02):
     return losses
 
 
+class Head:
+    """A frozen projection onto a vocabulary, on 4-bit weights."""
+
+    def __init__(self, vocab: int, d_model: int, seed: int = 1):
+        gen = torch.Generator(device="cuda").manual_seed(seed)
+        self.W, self.Wt = frozen_in_4_bits((torch.randn(vocab, d_model, generator=gen, device="cuda") / d_model ** 0.5).half())
+
+    def logits(self, y):
+        return lb.lordba_linear_i4(y, self.W)
+
+    def backward(self, d_logits):
+        return lb.lordba_linear_i4_backward(d_logits, self.Wt)
+
+
+def best(logits, k: int):
+    """A teacher's k best entries, as lordba_distill takes them."""
+    top = torch.topk(logits.float(), k, dim=1)
+    return top.indices.int(), top.values.to(logits.dtype)
+
+
+def distil_step(block: AdaptedBlock, head: Head, x, teacher, step: int, temperature: float = 2.0, kappa: float = 2.0):
+    """One pass through block, head and loss and back: the tokens' losses and the adapters' gradients of their mean, times 1024 (entries of the gradient with
+    respect to the logits are probabilities over the tokens' number: fp16 holds them so)."""
+    y, saved = block.forward(x, step)
+    logits = head.logits(y)
+    weight = torch.full((x.shape[0],), 1024.0 / x.shape[0], device=x.device)
+    loss, d_logits = lb.lordba_distill(logits, *teacher, temperature=temperature, d_loss=weight, d_logits_out=logits)
+    return loss, block.backward(head.backward(d_logits), saved, kappa)[1]
+
+
+def distil(block: AdaptedBlock, head: Head, x, teacher, steps: int, rate: float = 0.02):
+    """Gradient descent of the adapters on what the tokens lose against the teacher's top logits (top_index, top_logits); the mean loss of every step."""
+    losses = []
+    for step in range(steps):
+        loss, grads = distil_step(block, head, x, teacher, step)
+        losses.append(loss.mean().item())
+        for name, adapter in block.adapters.items():
+            adapter.step(grads[name], rate)
+    return losses
+
+
 def stronger(block: AdaptedBlock, x, factor: float = 2.0):
     """What the block answers with every branch `factor` times as large."""
     for a in block.adapters.values():
@@ -115,18 +187,24 @@ def stronger(block: AdaptedBlock, x, factor: float = 2.0):
 
 def main() -> None:
     p = argparse.ArgumentParser(description=__doc__.splitlines()[0])
-    for name, value in (("tokens", 512), ("d-model", 1024), ("d-ff", 2752), ("rank", 16), ("steps", 20)):
+    for name, value in (("tokens", 512), ("d-model", 1024), ("d-ff", 2752), ("rank", 16), ("steps", 20), ("bits", 8), ("vocab", 0), ("top", 16)):
         p.add_argument("--" + name, type=int, default=value)
     a = p.parse_args()
-    block = AdaptedBlock(a.d_model, a.d_ff, a.rank)
+    block = AdaptedBlock(a.d_model, a.d_ff, a.rank, bits=a.bits)
     gen = torch.Generator(device="cuda").manual_seed(1)
     x = torch.randn(a.tokens, a.d_model, generator=gen, device="cuda").half()
     target = stronger(block, x)
-    losses = fit(block, x, target, a.steps)
+    if a.vocab:
+        head = Head(a.vocab, a.d_model)
+        losses = distil(block, head, x, best(head.logits(target.half()), a.top), a.steps)
+    else:
+        losses = fit(block, x, target, a.steps)
     for k in range(0, a.steps, max(1, a.steps // 10)):
         print("step %3d  loss %.6f" % (k, losses[k]))
     print("step %3d  loss %.6f" % (a.steps - 1, losses[-1]))
     y = block.serve(x[:1].contiguous())
+    if a.vocab:
+        print("one token: best entry %d" % int(head.logits(y).argmax()))
     print("one token: |y| = %.4f, finite: %s" % (y.float().norm().item(), bool(torch.isfinite(y).all())))
 
 
