@@ -5,7 +5,8 @@
 
 namespace {
 
-constexpr int64_t kFewLds = 64 * 1024;   // what a workgroup keeps of the activations: two workgroups run on a compute unit side by side
+// What a workgroup of NW waves keeps of the activations: two of eight waves, or four of four, run on a compute unit side by side.
+constexpr int64_t few_lds(int NW) { return NW == 4 ? 32 * 1024 : 64 * 1024; }
 
 // A workgroup owns CB blocks of 16 weight rows (gated: half of them gate's, half up's) and up to 16 tokens; its NW waves share the contraction, wave w
 // taking the blocks of 128 columns w, w + NW, ...  The activations are kept in LDS, as many columns of them at a time as fit (`columns`, a multiple of 128),
@@ -15,7 +16,7 @@ constexpr int64_t kFewLds = 64 * 1024;   // what a workgroup keeps of the activa
 // multiplied by its scale in fp32, so that nothing is rounded but the sums.  Backward (S = 0): the scales vary along the contraction, so each weight is rounded
 // to fp16 before its product (half a step, 2^-11 of the weight).
 template <int CB, int NW, int D, int S, bool ZERO, bool GATED>
-__global__ __launch_bounds__(64 * NW, NW == 8 ? 4 : 1) void lordba_i4_few_kernel(I4Args a) {
+__global__ __launch_bounds__(64 * NW, NW <= 8 ? 4 : 1) void lordba_i4_few_kernel(I4Args a) {
     constexpr bool BWD = S == 0;
     constexpr int P = GATED ? 2 : 1, CT = CB / P;   // blocks of a half
     static_assert(CB % P == 0 && CT <= 2 && !(GATED && BWD), "a half's blocks lie in one pair: one group's rows in the transposed layout");
@@ -203,12 +204,12 @@ template <int CB, int NW, int D, int S, bool ZERO, bool GATED>
 lordba_status few_launch(I4Args a, hipStream_t stream) {
     constexpr int CT = CB / (GATED ? 2 : 1);
     // as many columns as fit, in equal parts, whole blocks for every wave where there are that many
-    const int64_t tokens = std::min<int64_t>(a.T, 16), most = kFewLds / (tokens * 256), parts = (a.blocks + most - 1) / most;
+    const int64_t tokens = std::min<int64_t>(a.T, 16), most = few_lds(NW) / (tokens * 256), parts = (a.blocks + most - 1) / most;
     int64_t blocks = (a.blocks + parts - 1) / parts;
     if (blocks > NW) blocks = std::min(most, (blocks + NW - 1) / NW * NW);
     a.columns = static_cast<int32_t>(blocks * kI4Columns);
     const size_t lds = static_cast<size_t>(std::max<int64_t>((tokens * blocks * 256 + 1023) / 1024 * 1024, NW * CB * 1024));   // (whole requests of 1 KiB)
-    static_assert(NW * CB * 1024 <= kFewLds, "room for the sums");
+    static_assert(NW * CB * 1024 <= few_lds(NW), "room for the sums");
     const int64_t n = (a.tiles + CT - 1) / CT * ((a.T + 15) / 16);
     constexpr int64_t kMost = (static_cast<int64_t>(1) << 31) / (64 * NW);   // (a launch counts threads in 32 bits)
     if (n > INT32_MAX) return LORDBA_ERR_DIM;
@@ -224,11 +225,13 @@ lordba_status few_launch(I4Args a, hipStream_t stream) {
 
 template <int S, bool ZERO, bool GATED>
 lordba_status few(const I4Args& a, hipStream_t stream) {
-    // Sixteen waves on a block of 16 rows where there are no more blocks than compute units; with more, two workgroups of eight waves on each, and two blocks
-    // of rows a workgroup where that many tokens make the staging of the activations the larger part: one token 4096 -> 11008 10.2 us with sixteen
-    // waves, 7.8 with eight, 7.8 on two blocks, 16 tokens 21, 18.5, 14.8; one token 11008 -> 4096 7.2 us with sixteen, 9.1 on two blocks.
-    // Backward, where a wave's scales take as many registers as its codes, eight waves throughout (16 x 4096 -> 4096 10.6 -> 8.8 us).
+    // More blocks of 16 rows than two workgroups of eight waves on every compute unit: four waves, and four workgroups side by side (one token 4096 -> 11008
+    // 6.8 us, with eight waves 7.8; 301 -> 13001 4.6 and 6.4; gated 4096 -> 11008 12.8 and 15.4).  No more than compute units: sixteen waves on each (one token
+    // 13001 -> 301 6.7, with eight 7.1, with four 9.0), but backward, where a wave's scales take as many registers as its codes, eight (16 x 4096 -> 4096 8.8,
+    // with sixteen 10.6).  Between them, and with more tokens, whose staging then is the larger part, eight waves, on two blocks of rows (16 x 4096 -> 11008 18.5 ->
+    // 14.8 us).
     constexpr int P = GATED ? 2 : 1, D = S == 0 || S == 4 ? 2 : 4;
+    if (a.tiles > 512 && a.T <= 8) return few_launch<P, 4, D, S, ZERO, GATED>(a, stream);
     if constexpr (S > 0 && !GATED) {
         if (a.tiles * ((a.T + 15) / 16) <= 256) return few_launch<1, 16, 2, S, ZERO, GATED>(a, stream);
     }

@@ -25,7 +25,7 @@ SHAPES = [(1, 1, 1, 32, True), (1, 128, 32, 128, False), (2, 31, 33, 32, True), 
           (32, 3328, 520, 128, True), (48, 2050, 1001, 64, False), (96, 2048, 1024, 32, True), (256, 1288, 4136, 128, False), (300, 1032, 1032, 32, True),
           (260, 5000, 264, 64, True), (640, 2056, 1536, 64, True), (1500, 520, 2056, 128, False), (1024, 1024, 4096, 32, False), (1100, 4104, 776, 128, True),
           (4100, 264, 520, 64, True), (2500, 1025, 700, 32, True), (40, 4104, 2072, 64, True), (64, 8192, 2048, 32, False), (60, 8200, 2051, 128, True),
-          (61, 8264, 1991, 64, False)]
+          (61, 8264, 1991, 64, False), (3, 300, 8300, 128, True), (8, 1030, 8321, 32, False), (1, 8400, 264, 64, True), (7, 8320, 130, 128, False)]
 
 
 @functools.lru_cache(None)
