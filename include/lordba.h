@@ -41,7 +41,7 @@ enum {
     LORDBA_ERR_DIM = 2,       /* T < 0, d_in < 1, d_out < 1, r < 1, r > LORDBA_MAX_RANK, or a
                                  size that does not fit 32-bit indexing of one row             */
     LORDBA_ERR_VALUE = 3,     /* a sign entry that is not +-1 (int8 variant) or is NaN (f32); a parameter
-                                 outside its range (tau, mu, digits, p, group, halves, temperature, type) */
+                                 outside its range (tau, mu, digits, p, group, halves, type, temperature) */
     LORDBA_ERR_ALIAS = 4,     /* y_out overlaps an input other than being exactly y_base      */
     LORDBA_ERR_ALIGN = 5,     /* a pointer is not aligned to its element size                 */
     LORDBA_ERR_NO_DEVICE = 6, /* no usable HIP device / not a gfx950 device                   */
@@ -499,12 +499,12 @@ lordba_status lordba_dropout(const void* x, const void* y_base, void* y_out, int
  *     W[j, i] = scale[j, i / group] * (code[j, i] - zero[j, i / group]),   group = 32, 64 or 128 columns of a row,
  * codes and zeros whole numbers from 0 to 15 (their low four bits count; zeros that are not given are 8), scales finite fp16 numbers.  Activations, results and
  * gradients are fp16.  Sums are held in fp32 and rounded once.
- *     up to LORDBA_I4_FEW tokens, forward: a group's sum of x * (code - zero), each factor exact, is multiplied by its scale in fp32
- *     more tokens, and every gradient: scale * (code - zero) is rounded to fp16 first, half a step (2^-11 of the weight) at most: relative to the norms of
+ *     forward, up to 8 tokens (and more of them where that takes less time): a group's sum of x * (code - zero), each factor exact, is multiplied by its
+ *     scale in fp32
+ *     forward with more, and every gradient: scale * (code - zero) is rounded to fp16 first, half a step (2^-11 of the weight) at most: relative to the norms of
  *     what is summed 1.7e-4 in the root mean square, beside 2.1e-4 from the rounding of the result.  So |15 scale| has to be in the range of fp16.
  * lordba_quantize_i4 makes codes and scales from fp16 weights, lordba_layout_i4 brings them once into the form that the products read, as W or as its
  * transpose (for the gradients).  The matrices of the gated block have two halves, gate's rows and then up's. */
-#define LORDBA_I4_FEW 64
 
 /* Bytes of the laid-out codes of a matrix W [rows, cols], and the number of fp16 scales (and of zeros) that go with them; 0 for arguments out of range.
  * rows, cols <= 2^24; halves: 1, or 2 with an even number of rows; transposed: the layout of W's transpose. */
