@@ -1170,11 +1170,12 @@ def lordba_layout_i4(codes, scale, zero=None, group: int = 128, halves: int = 1,
     return WeightsI4(out, out_scale, out_zero, rows, cols, group, halves, bool(transposed))
 
 
-def _weights_i4(W, halves: int, transposed: bool, what: str) -> None:
+def _weights_i4(W, halves: int, transposed: bool, what: str) -> WeightsI4:
     import torch
 
-    if not isinstance(W, WeightsI4):
+    if not isinstance(W, tuple) or len(W) != len(WeightsI4._fields):
         raise TypeError("%s must be what lordba_layout_i4 returns" % what)
+    W = WeightsI4(*W)
     if W.halves != halves or bool(W.transposed) is not transposed:
         raise ValueError("%s must be laid out with halves=%d, transposed=%s" % (what, halves, transposed))
     lib = load_library()
@@ -1186,6 +1187,7 @@ def _weights_i4(W, halves: int, transposed: bool, what: str) -> None:
     if n == 0 or W.codes.numel() != lib.lordba_i4_code_bytes(W.rows, W.cols, halves, int(transposed)) or W.scale.numel() != n or \
             (W.zero is not None and W.zero.numel() != n):
         raise ValueError("%s is not the layout of its sizes" % what)
+    return W
 
 
 def _linear_i4(name: str, x, W, y_out, stream, backward: bool):
@@ -1193,7 +1195,7 @@ def _linear_i4(name: str, x, W, y_out, stream, backward: bool):
 
     lib = load_library()
     _need(torch.float16, "float16 CUDA tensor", ("g" if backward else "x",), x)
-    _weights_i4(W, 1, backward, "Wt" if backward else "W")
+    W = _weights_i4(W, 1, backward, "Wt" if backward else "W")
     k, n = (W.rows, W.cols) if backward else (W.cols, W.rows)
     if x.dim() != 2 or x.shape[1] != k:
         raise ValueError("%s must be [T, %d]" % ("g" if backward else "x", k))
@@ -1232,7 +1234,7 @@ def lordba_gated_i4(x, W: WeightsI4, addends=None, save: bool = False, stream=No
 
     lib = load_library()
     _need(torch.float16, "float16 CUDA tensor", ("x",), x)
-    _weights_i4(W, 2, False, "W")
+    W = _weights_i4(W, 2, False, "W")
     if x.dim() != 2 or x.shape[1] != W.cols:
         raise ValueError("x must be [T, %d]" % W.cols)
     T, d_in = x.shape
@@ -1262,7 +1264,7 @@ def lordba_gated_i4_backward(dh, gate_up, Wt: WeightsI4, stream=None):
 
     lib = load_library()
     _need(torch.float16, "float16 CUDA tensor", ("dh", "gate_up"), dh, gate_up)
-    _weights_i4(Wt, 2, True, "Wt")
+    Wt = _weights_i4(Wt, 2, True, "Wt")
     if dh.dim() != 2 or 2 * dh.shape[1] != Wt.rows or tuple(gate_up.shape) != (2,) + tuple(dh.shape):
         raise ValueError("dh must be [T, %d], gate_up [2, T, %d]" % (Wt.rows // 2, Wt.rows // 2))
     T, d_ff = dh.shape

@@ -76,8 +76,10 @@ __global__ __launch_bounds__(256) void lordba_layout_i4_kernel(LayoutArgs a) {
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
             int64_t j, i;
-            uint32_t code = 8;
+            uint32_t code = 8;   // (stands for 0 where the scale is padding too)
             if (source(a, tile, lane & 15, c0 + e, j, i)) code = a.codes[j * a.cols + i] & 15u;
+            // behind the end of a row, in a group that it has: the group's zero
+            else if (!a.transposed && a.zero && c0 + e < a.groups * a.group && source(a, tile, lane & 15, 0, j, i)) code = a.zero[j * a.groups + (c0 + e) / a.group] & 15u;
             v |= code << (4 * i4_nibble(e));
         }
         a.out[k] = v;

@@ -120,6 +120,30 @@ def test_rows_that_hold_no_numbers_spoil_no_others(torch, T, d_in):
     assert bool(torch.isnan(dx2[1]).all())
 
 
+@pytest.mark.parametrize("T", [2, 100])
+@pytest.mark.parametrize("d_in", [200, 201])
+def test_padding_behind_large_scales(torch, T, d_in):
+    # weights of 0 under scales whose other multiples pass the range of fp16: nothing behind a row's end comes into its sums
+    codes = torch.full((40, d_in), 3, dtype=torch.uint8, device="cuda")
+    scale = torch.full((40, -(-d_in // 128)), 60000.0, dtype=torch.float16, device="cuda")
+    zero = torch.full(scale.shape, 3, dtype=torch.uint8, device="cuda")
+    x = torch.randn(T, d_in, device="cuda").half()
+    y = binding.lordba_linear_i4(x, binding.lordba_layout_i4(codes, scale, zero))
+    assert bool((y == 0).all())
+
+
+def test_a_tuple_will_do(torch):
+    codes, scale, zero = binding.lordba_quantize_i4(torch.randn(64, 96, device="cuda").half(), 32, True)
+    W, x = binding.lordba_layout_i4(codes, scale, zero, 32), torch.randn(5, 96, device="cuda").half()
+    y = binding.lordba_linear_i4(x, W)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    for W2, stream in ((tuple(W), None), (tuple(W), side)):
+        y2 = binding.lordba_linear_i4(x, W2, stream=stream)
+        torch.cuda.synchronize()
+        assert torch.equal(y2, y)
+
+
 def test_no_tokens(torch):
     codes, scale, _ = binding.lordba_quantize_i4(torch.randn(64, 96, device="cuda").half(), 32)
     x, g = torch.empty(0, 96, dtype=torch.float16, device="cuda"), torch.empty(0, 64, dtype=torch.float16, device="cuda")
