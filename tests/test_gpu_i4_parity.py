@@ -155,7 +155,7 @@ def test_no_tokens(torch):
 
 
 @pytest.mark.parametrize("zero_points", [False, True])
-@pytest.mark.parametrize("group,rows,cols", [(32, 5, 33), (64, 70, 200), (128, 33, 1000), (128, 1, 1)])
+@pytest.mark.parametrize("group,rows,cols", [(32, 5, 33), (64, 70, 200), (128, 33, 1000), (128, 4, 9), (128, 1, 1)])
 def test_quantiser(torch, group, rows, cols, zero_points):
     rng = np.random.default_rng(cols)
     w = rng.standard_normal((rows, cols)).astype(np.float16)
