@@ -504,7 +504,8 @@ lordba_status lordba_dropout(const void* x, const void* y_base, void* y_out, int
  *     forward with more, and every gradient: scale * (code - zero) is rounded to fp16 first, half a step (2^-11 of the weight) at most: relative to the norms of
  *     what is summed 1.7e-4 in the root mean square, beside 2.1e-4 from the rounding of the result.  So |15 scale| has to be in the range of fp16.
  * lordba_quantize_i4 makes codes and scales from fp16 weights, lordba_layout_i4 brings them once into the form that the products read, as W or as its
- * transpose (for the gradients).  The matrices of the gated block have two halves, gate's rows and then up's. */
+ * transpose (for the gradients).  The matrices of the gated block have two halves, gate's rows and then up's.
+ * Here and in the calls below all memory and the stream belong to the current device. */
 
 /* Bytes of the laid-out codes of a matrix W [rows, cols], and the number of fp16 scales (and of zeros) that go with them; 0 for arguments out of range.
  * rows, cols <= 2^24; halves: 1, or 2 with an even number of rows; transposed: the layout of W's transpose. */
@@ -544,7 +545,8 @@ lordba_status lordba_gated_i4(const void* x, const uint8_t* codes, const void* s
 /* DEVICE function: its backward pass, from dh fp16 [T, d_ff] and the kept gate_up:
  *     dgate = dh * up * sigma(gate) * (1 + gate * (1 - sigma(gate))),  dup = dh * gate * sigma(gate),  dx = dgate Wg + dup Wu
  * with the transposed layout of W [2 d_ff, d_in] in two halves; dx fp16 [T, d_in]; dgate_up fp16 [2, T, d_ff]: dgate and dup, of which, rounded, dx is
- * made.  Everything else as lordba_linear_i4. */
+ * made: the matrix instructions take 16-bit numbers, and two of them for each would take twice the time (relative to the norm of dx 3.4e-4, with the
+ * rounding of the weights and of dx; 2.1e-4 is that of dx alone).  Everything else as lordba_linear_i4. */
 lordba_status lordba_gated_i4_backward(const void* dh, const void* gate_up, const uint8_t* codes_t, const void* scale_t, const void* zero_t, void* dx,
                                        void* dgate_up, int64_t T, int64_t d_in, int64_t d_ff, int64_t group, void* stream);
 

@@ -1113,6 +1113,17 @@ class WeightsI4(NamedTuple):
     transposed: bool
 
 
+@contextlib.contextmanager
+def _on_device(stream, first, *others):
+    """Where the calls below run: on the device of their tensors, which has to be one, whichever is the current one; outputs are made on the stream."""
+    import torch
+
+    if any(t_ is not None and t_.device != first.device for t_ in others):
+        raise ValueError("all tensors must be on one device")
+    with torch.cuda.device(first.device), _on_stream(stream):
+        yield
+
+
 def lordba_quantize_i4(w, group: int = 128, zero_points: bool = False, stream=None):
     """fp16 weights w [rows, cols] on 4 bits: (codes uint8 [rows, cols], scale fp16 [rows, groups], zero uint8 [rows, groups] or None) with
     w ~ scale * (code - zero) for every `group` columns of a row, zero 8 where None; zero_points: the range of a group from its smallest to its largest."""
@@ -1125,12 +1136,12 @@ def lordba_quantize_i4(w, group: int = 128, zero_points: bool = False, stream=No
     if group not in (32, 64, 128):
         raise ValueError("group must be 32, 64 or 128")
     rows, cols = w.shape
-    with _on_stream(stream):
+    with _on_device(stream, w):
         codes = torch.empty((rows, cols), dtype=torch.uint8, device=w.device)
         scale = torch.empty((rows, -(-cols // group)), dtype=torch.float16, device=w.device)
         zero = torch.empty(scale.shape, dtype=torch.uint8, device=w.device) if zero_points else None
-    st = lib.lordba_quantize_i4(w.data_ptr(), codes.data_ptr(), scale.data_ptr(), None if zero is None else zero.data_ptr(), rows, cols, group,
-                                _stream_handle(w, stream))
+        st = lib.lordba_quantize_i4(w.data_ptr(), codes.data_ptr(), scale.data_ptr(), None if zero is None else zero.data_ptr(), rows, cols, group,
+                                    _stream_handle(w, stream))
     if st != 0:
         raise LordbaError(st, "lordba_quantize_i4")
     return codes, scale, zero
@@ -1158,13 +1169,13 @@ def lordba_layout_i4(codes, scale, zero=None, group: int = 128, halves: int = 1,
         if zero.shape != scale.shape:
             raise ValueError("zero must be [rows, groups]")
     n = lib.lordba_i4_scale_count(rows, cols, group, halves, int(bool(transposed)))
-    with _on_stream(stream):
+    with _on_device(stream, codes, scale, zero):
         out = torch.empty(lib.lordba_i4_code_bytes(rows, cols, halves, int(bool(transposed))), dtype=torch.uint8, device=codes.device)
         out_scale = torch.empty(n, dtype=torch.float16, device=codes.device)
         out_zero = None if zero is None else torch.empty_like(out_scale)
-    ptr = lambda t_: None if t_ is None else t_.data_ptr()
-    st = lib.lordba_layout_i4(codes.data_ptr(), scale.data_ptr(), ptr(zero), out.data_ptr(), out_scale.data_ptr(), ptr(out_zero), rows, cols, group, halves,
-                              int(bool(transposed)), _stream_handle(codes, stream))
+        ptr = lambda t_: None if t_ is None else t_.data_ptr()
+        st = lib.lordba_layout_i4(codes.data_ptr(), scale.data_ptr(), ptr(zero), out.data_ptr(), out_scale.data_ptr(), ptr(out_zero), rows, cols, group, halves,
+                                  int(bool(transposed)), _stream_handle(codes, stream))
     if st != 0:
         raise LordbaError(st, "lordba_layout_i4")
     return WeightsI4(out, out_scale, out_zero, rows, cols, group, halves, bool(transposed))
@@ -1200,10 +1211,10 @@ def _linear_i4(name: str, x, W, y_out, stream, backward: bool):
     if x.dim() != 2 or x.shape[1] != k:
         raise ValueError("%s must be [T, %d]" % ("g" if backward else "x", k))
     T = x.shape[0]
-    with _on_stream(stream):
+    with _on_device(stream, x, W.codes, W.scale, W.zero, y_out):
         y_out = _output(y_out, (T, n), x, "dx_out" if backward else "y_out")
-    st = getattr(lib, name)(x.data_ptr(), W.codes.data_ptr(), W.scale.data_ptr(), None if W.zero is None else W.zero.data_ptr(), y_out.data_ptr(), T,
-                            W.cols, W.rows, W.group, _stream_handle(x, stream))
+        st = getattr(lib, name)(x.data_ptr(), W.codes.data_ptr(), W.scale.data_ptr(), None if W.zero is None else W.zero.data_ptr(), y_out.data_ptr(), T,
+                                W.cols, W.rows, W.group, _stream_handle(x, stream))
     if st != 0:
         raise LordbaError(st, name)
     return y_out
@@ -1243,12 +1254,12 @@ def lordba_gated_i4(x, W: WeightsI4, addends=None, save: bool = False, stream=No
         _need(torch.float16, "float16 CUDA tensor", ("addends",), addends)
         if tuple(addends.shape) != (2, T, d_ff):
             raise ValueError("addends must be [2, T, d_ff]")
-    with _on_stream(stream):
+    with _on_device(stream, x, W.codes, W.scale, W.zero, addends):
         h = _output(None, (T, d_ff), x, "h")
         gate_up = _output(None, (2, T, d_ff), x, "gate_up") if save else None
-    ptr = lambda t_: None if t_ is None else t_.data_ptr()
-    st = lib.lordba_gated_i4(x.data_ptr(), W.codes.data_ptr(), W.scale.data_ptr(), ptr(W.zero), ptr(addends), h.data_ptr(), ptr(gate_up), T, d_in, d_ff,
-                             W.group, _stream_handle(x, stream))
+        ptr = lambda t_: None if t_ is None else t_.data_ptr()
+        st = lib.lordba_gated_i4(x.data_ptr(), W.codes.data_ptr(), W.scale.data_ptr(), ptr(W.zero), ptr(addends), h.data_ptr(), ptr(gate_up), T, d_in, d_ff,
+                                 W.group, _stream_handle(x, stream))
     if st != 0:
         raise LordbaError(st, "lordba_gated_i4")
     return (h, gate_up) if save else h
@@ -1269,11 +1280,11 @@ def lordba_gated_i4_backward(dh, gate_up, Wt: WeightsI4, stream=None):
         raise ValueError("dh must be [T, %d], gate_up [2, T, %d]" % (Wt.rows // 2, Wt.rows // 2))
     T, d_ff = dh.shape
     d_in = Wt.cols
-    with _on_stream(stream):
+    with _on_device(stream, dh, gate_up, Wt.codes, Wt.scale, Wt.zero):
         dx, dgate_up = _output(None, (T, d_in), dh, "dx"), _output(None, (2, T, d_ff), dh, "dgate_up")
-    st = lib.lordba_gated_i4_backward(dh.data_ptr(), gate_up.data_ptr(), Wt.codes.data_ptr(), Wt.scale.data_ptr(),
-                                      None if Wt.zero is None else Wt.zero.data_ptr(), dx.data_ptr(), dgate_up.data_ptr(), T, d_in, d_ff, Wt.group,
-                                      _stream_handle(dh, stream))
+        st = lib.lordba_gated_i4_backward(dh.data_ptr(), gate_up.data_ptr(), Wt.codes.data_ptr(), Wt.scale.data_ptr(),
+                                          None if Wt.zero is None else Wt.zero.data_ptr(), dx.data_ptr(), dgate_up.data_ptr(), T, d_in, d_ff, Wt.group,
+                                          _stream_handle(dh, stream))
     if st != 0:
         raise LordbaError(st, "lordba_gated_i4_backward")
     return dx, dgate_up
@@ -1343,13 +1354,13 @@ def lordba_distill(logits, top_index=None, top_logits=None, labels=None, tempera
         raise ValueError("d_logits_out needs d_loss")
     if d_loss is not None:
         _per_token(d_loss, T, "d_loss")
-    with _on_stream(stream):
+    with _on_device(stream, logits, top_index, top_logits, labels, d_loss, d_logits_out):
         loss = torch.empty(T, dtype=torch.float32, device=logits.device)
         kept = torch.empty((T, 3), dtype=torch.float32, device=logits.device) if d_loss is None else None
         d_logits = None if d_loss is None else _logits_out(d_logits_out, logits)
-    ptr = lambda t_: None if t_ is None else t_.data_ptr()
-    st = lib.lordba_distill(logits.data_ptr(), int(logits.dtype is torch.float32), ctypes.byref(teacher), ptr(d_loss), loss.data_ptr(), ptr(kept), ptr(d_logits),
-                            T, V, _stream_handle(logits, stream))
+        ptr = lambda t_: None if t_ is None else t_.data_ptr()
+        st = lib.lordba_distill(logits.data_ptr(), int(logits.dtype is torch.float32), ctypes.byref(teacher), ptr(d_loss), loss.data_ptr(), ptr(kept), ptr(d_logits),
+                                T, V, _stream_handle(logits, stream))
     if st != 0:
         raise LordbaError(st, "lordba_distill")
     return loss, kept if d_loss is None else d_logits
@@ -1371,10 +1382,10 @@ def lordba_distill_backward(d_loss, logits, kept, top_index=None, top_logits=Non
     _need(torch.float32, "float32 CUDA tensor", ("kept",), kept)
     if tuple(kept.shape) != (T, 3):
         raise ValueError("kept must be [T, 3]")
-    with _on_stream(stream):
+    with _on_device(stream, logits, d_loss, kept, top_index, top_logits, labels, d_logits_out):
         d_logits_out = _logits_out(d_logits_out, logits)
-    st = lib.lordba_distill_backward(d_loss.data_ptr(), logits.data_ptr(), int(logits.dtype is torch.float32), kept.data_ptr(), ctypes.byref(teacher),
-                                     d_logits_out.data_ptr(), T, V, _stream_handle(logits, stream))
+        st = lib.lordba_distill_backward(d_loss.data_ptr(), logits.data_ptr(), int(logits.dtype is torch.float32), kept.data_ptr(), ctypes.byref(teacher),
+                                         d_logits_out.data_ptr(), T, V, _stream_handle(logits, stream))
     if st != 0:
         raise LordbaError(st, "lordba_distill_backward")
     return d_logits_out

@@ -10,6 +10,7 @@
 #include <ATen/ATen.h>
 #include <ATen/PythonTorchFunctionTLS.h>
 #include <c10/core/impl/TorchDispatchModeTLS.h>
+#include <c10/hip/HIPFunctions.h>
 #include <c10/hip/HIPStream.h>
 #include <torch/csrc/Exceptions.h>
 #include <torch/csrc/PyInterpreter.h>
@@ -451,6 +452,14 @@ PyObject* dropout(PyObject*, PyObject* const* a, Py_ssize_t n) {
 }
 
 // ---- 4-bit projections, learning from a teacher.
+// Everything on the current device (another one the binding makes current first, or refuses).
+bool here(std::initializer_list<const at::Tensor*> all) {
+    const auto device = c10::hip::current_device();
+    for (const at::Tensor* t : all)
+        if (t && t->get_device() != device) return false;
+    return true;
+}
+
 struct WeightsI4 {   // the named tuple of the binding: codes, scale, zero or None, rows, cols, group, halves, transposed
     const at::Tensor *codes, *scale, *zero;
     int64_t rows, cols, group;
@@ -479,11 +488,11 @@ PyObject* linear_i4_any(PyObject* const* a, Py_ssize_t n, bool backward) {
     NEED(n == 4 && unwatched() && a[3] == Py_None);
     const at::Tensor* x = plain(a[0], kF16);
     WeightsI4 w;
-    NEED(x && x->dim() == 2 && w.read(a[1], 1, backward) && x->size(1) == (backward ? w.rows : w.cols));
+    NEED(x && x->dim() == 2 && w.read(a[1], 1, backward) && here({x, w.codes, w.scale, w.zero}) && x->size(1) == (backward ? w.rows : w.cols));
     const int64_t T = x->size(0);
     void* st;
     at::Tensor y;
-    NEED(stream_of(a[3], x, &st) && tensor_or_new(a[2], kF16, x, {T, backward ? w.cols : w.rows}, false, &y));
+    NEED(stream_of(a[3], x, &st) && tensor_or_new(a[2], kF16, x, {T, backward ? w.cols : w.rows}, false, &y) && here({&y}));
     const int rc = unlocked(backward ? lordba_linear_i4_backward : lordba_linear_i4, ptr<void>(x), ptr<uint8_t>(w.codes), ptr<void>(w.scale),
                             ptr<void>(w.zero), ptr<void>(y), T, w.cols, w.rows, w.group, st);
     return result(y, rc);
@@ -505,7 +514,7 @@ PyObject* gated_i4(PyObject*, PyObject* const* a, Py_ssize_t n) {
     NEED(n == 5 && unwatched() && a[4] == Py_None && (a[3] == Py_True || a[3] == Py_False));
     const at::Tensor *x = plain(a[0], kF16), *add = a[2] == Py_None ? nullptr : plain(a[2], kF16);
     WeightsI4 w;
-    NEED(x && (add || a[2] == Py_None) && x->dim() == 2 && w.read(a[1], 2, false) && x->size(1) == w.cols);
+    NEED(x && (add || a[2] == Py_None) && x->dim() == 2 && w.read(a[1], 2, false) && here({x, w.codes, w.scale, w.zero, add}) && x->size(1) == w.cols);
     const int64_t T = x->size(0), F = w.rows / 2;
     NEED(!add || shaped(add, {2, T, F}));
     void* st;
@@ -525,7 +534,7 @@ PyObject* gated_i4_backward(PyObject*, PyObject* const* a, Py_ssize_t n) {
     NEED(n == 4 && unwatched() && a[3] == Py_None);
     const at::Tensor *dh = plain(a[0], kF16), *gu = plain(a[1], kF16);
     WeightsI4 w;
-    NEED(dh && gu && dh->dim() == 2 && w.read(a[2], 2, true) && 2 * dh->size(1) == w.rows);
+    NEED(dh && gu && dh->dim() == 2 && w.read(a[2], 2, true) && here({dh, gu, w.codes, w.scale, w.zero}) && 2 * dh->size(1) == w.rows);
     const int64_t T = dh->size(0), F = dh->size(1);
     NEED(shaped(gu, {2, T, F}));
     void* st;
@@ -551,7 +560,7 @@ struct Distill {   // what both calls share: logits; top_index, top_logits, labe
                          *labels = a[2] == Py_None ? nullptr : plain(a[2], kI32);
         if ((!index && a[0] != Py_None) || (!top && a[1] != Py_None) || (!labels && a[2] != Py_None) || !index != !top) return false;
         if (index && (index->dim() != 2 || index->size(0) != T || top->sizes() != index->sizes())) return false;
-        if (labels && !shaped(labels, {T})) return false;
+        if ((labels && !shaped(labels, {T})) || !here({z, index, top, labels})) return false;
         w.k = index ? index->size(1) : 0;
         w.top_index = ptr<int32_t>(index), w.top_logits = ptr<void>(top), w.labels = ptr<int32_t>(labels);
         return number(a[3], &w.temperature) && number(a[4], &w.soft) && number(a[5], &w.hard);
@@ -564,10 +573,10 @@ PyObject* distill(PyObject*, PyObject* const* a, Py_ssize_t n) {
     Distill d;
     NEED(n == 10 && unwatched() && a[9] == Py_None && d.read(a[0], a + 1));
     const at::Tensor* weight = a[7] == Py_None ? nullptr : plain(a[7], kF32);
-    NEED((weight && shaped(weight, {d.T})) || (a[7] == Py_None && a[8] == Py_None));
+    NEED((weight && here({weight}) && shaped(weight, {d.T})) || (a[7] == Py_None && a[8] == Py_None));
     void* st;
     at::Tensor grad, kept;
-    NEED(stream_of(a[9], d.z, &st) && (!weight || tensor_or_new(a[8], d.z->scalar_type(), d.z, d.z->sizes(), false, &grad)));
+    NEED(stream_of(a[9], d.z, &st) && (!weight || (tensor_or_new(a[8], d.z->scalar_type(), d.z, d.z->sizes(), false, &grad) && here({&grad}))));
     const at::Tensor loss = empty(d.z, kF32, {d.T});
     if (!weight) kept = empty(d.z, kF32, {d.T, 3});
     const int rc = unlocked(lordba_distill, ptr<void>(d.z), d.type, &d.w, ptr<float>(weight), ptr<float>(loss), weight ? nullptr : ptr<float>(kept),
@@ -582,10 +591,10 @@ PyObject* distill_backward(PyObject*, PyObject* const* a, Py_ssize_t n) {
     Distill d;
     NEED(n == 11 && unwatched() && a[10] == Py_None && d.read(a[1], a + 3));
     const at::Tensor *weight = plain(a[0], kF32), *kept = plain(a[2], kF32);
-    NEED(weight && kept && shaped(weight, {d.T}) && shaped(kept, {d.T, 3}));
+    NEED(weight && kept && here({weight, kept}) && shaped(weight, {d.T}) && shaped(kept, {d.T, 3}));
     void* st;
     at::Tensor grad;
-    NEED(stream_of(a[10], d.z, &st) && tensor_or_new(a[9], d.z->scalar_type(), d.z, d.z->sizes(), false, &grad));
+    NEED(stream_of(a[10], d.z, &st) && tensor_or_new(a[9], d.z->scalar_type(), d.z, d.z->sizes(), false, &grad) && here({&grad}));
     const int rc = unlocked(lordba_distill_backward, ptr<float>(weight), ptr<void>(d.z), d.type, ptr<float>(kept), &d.w, ptr<void>(grad), d.T, d.V, st);
     return result(grad, rc);
     END_HANDLE_TH_ERRORS

@@ -157,6 +157,22 @@ def test_infinities_and_empty_rows(torch, wide):
     assert float(loss) == inf and bool(torch.isfinite(grad).all()) and float(grad[0, 0]) < 0
 
 
+def test_more_tokens_than_one_launch_takes(torch):
+    T, V = (1 << 24) + 1000, 3
+    z = torch.randn(T, V, device="cuda", generator=torch.Generator("cuda").manual_seed(3))
+    index = (torch.arange(T, device="cuda", dtype=torch.int32) % V)[:, None].contiguous()
+    loss, grad = binding.lordba_distill(z, index, torch.zeros(T, 1, device="cuda"), d_loss=torch.ones(T, device="cuda"))
+    log_q = torch.log_softmax(z.double(), 1)
+    want = -log_q.gather(1, index.long())[:, 0]      # (one entry: p = 1)
+    A = (z.amax(1) - z.amin(1)).double() + np.log(V)
+    assert bool((abs(loss - want) <= 1.01 * (rel(V, A) + want * (rel(V, A) + 2.0 ** -21)) + want * 2.0 ** -23).all())
+    want = log_q.exp()
+    err = want * (rel(V, A) + 2.0 ** -21)[:, None]
+    want.scatter_add_(1, index.long(), -torch.ones(T, 1, dtype=torch.float64, device="cuda"))
+    err.scatter_add_(1, index.long(), (rel(1024, A) + 2.0 ** -21)[:, None])
+    assert bool((abs(grad - want) <= 1.01 * err + abs(want) * 2.0 ** -23).all())
+
+
 def test_differences(torch):
     # central differences of the loss: off by h^2 / 6 times the third derivative (for each term at most 1 / u^3 of its factor u^2, 1) and by the loss's error / h
     V, k, u, soft, hard, h = 40, 6, 2.0, 1.0, 0.5, 2.0 ** -5

@@ -144,6 +144,38 @@ def test_a_tuple_will_do(torch):
         assert torch.equal(y2, y)
 
 
+def test_more_workgroups_than_one_launch_takes(torch):
+    # and results behind the first 2^32 bytes
+    T, d_in, d_out = 300001, 5, 8192
+    rng = np.random.default_rng(4)
+    codes, scale, zero = i4_checks.weights(torch, rng, d_out, d_in, 32, True)
+    W = i4_checks.real(torch, codes, scale, zero, 32, rounded=False).cuda()
+    x = torch.randn(T, d_in, device="cuda", generator=torch.Generator("cuda").manual_seed(4)).half()
+    y = binding.lordba_linear_i4(x, binding.lordba_layout_i4(codes.cuda(), scale.cuda(), zero.cuda(), 32))
+    for t in range(0, T, 10000):
+        i8_checks.near(y[t:t + 10000], *i4_checks.product(torch, x[t:t + 10000].double(), W))
+
+
+@pytest.mark.parametrize("T,k,n", [(40, 1 << 22, 24), (40, (1 << 22) + 8, 24), (3, (1 << 22) + 1, 24)])
+@pytest.mark.parametrize("backward", [False, True])
+def test_long_contractions(torch, T, k, n, backward):
+    rng = np.random.default_rng(k + T)
+    codes, scale, zero = i4_checks.weights(torch, rng, *((k, n) if backward else (n, k)), 128, True)
+    W = i4_checks.real(torch, codes, scale, zero, 128, rounded=backward or i4_checks.kernel(T, k, n) != "few").cuda()
+    x = torch.randn(T, k, device="cuda", generator=torch.Generator("cuda").manual_seed(T)).half()
+    laid = binding.lordba_layout_i4(codes.cuda(), scale.cuda(), zero.cuda(), transposed=backward)
+    y = binding.lordba_linear_i4_backward(x, laid) if backward else binding.lordba_linear_i4(x, laid)
+    i8_checks.near(y, *i4_checks.product(torch, x.double(), W.t().contiguous() if backward else W))
+
+
+def test_the_low_four_bits_count(torch):
+    codes, scale, zero = binding.lordba_quantize_i4(torch.randn(64, 200, device="cuda").half(), 64, True)
+    for transposed in (False, True):
+        a = binding.lordba_layout_i4(codes, scale, zero, 64, transposed=transposed)
+        b = binding.lordba_layout_i4(codes ^ 0xf0, scale, zero ^ 0xf0, 64, transposed=transposed)
+        assert torch.equal(a.codes, b.codes) and torch.equal(a.scale, b.scale) and torch.equal(a.zero, b.zero)
+
+
 def test_no_tokens(torch):
     codes, scale, _ = binding.lordba_quantize_i4(torch.randn(64, 96, device="cuda").half(), 32)
     x, g = torch.empty(0, 96, dtype=torch.float16, device="cuda"), torch.empty(0, 64, dtype=torch.float16, device="cuda")

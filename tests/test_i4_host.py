@@ -151,3 +151,13 @@ def test_what_the_binding_refuses():
     for name, n in (("linear_i4", 4), ("linear_i4_backward", 4), ("gated_i4", 5), ("gated_i4_backward", 4), ("distill", 10), ("distill_backward", 11)):
         f = getattr(m, name)      # what is not plain is left to the binding
         assert f(*[half] * n) is None and f(*[None] * n) is None and f(*["x"] * n) is None and f(*[W] * n) is None and f(half) is None, name
+
+
+def test_tensors_of_two_devices_are_refused():
+    class On:
+        def __init__(self, device):
+            self.device = torch.device("cuda", device)
+
+    with pytest.raises(ValueError, match="one device"):
+        with binding._on_device(None, On(0), None, On(0), On(1)):
+            pass
