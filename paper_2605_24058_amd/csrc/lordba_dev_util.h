@@ -58,13 +58,6 @@ __device__ __forceinline__ void load16_to_lds(uint32_t lds, const void* p) {
     if constexpr (STREAM) asm volatile("s_nop 0\n\tglobal_load_lds_dwordx4 %0, off nt" :: "v"(p), "{m0}"(lds) : "memory");
     else asm volatile("s_nop 0\n\tglobal_load_lds_dwordx4 %0, off" :: "v"(p), "{m0}"(lds) : "memory");
 }
-// The same from a uniform base and a byte offset per lane.
-__device__ __forceinline__ void load16_to_lds_from(uint32_t lds, const void* base, uint32_t byte_off) {
-    const uint64_t b = reinterpret_cast<uint64_t>(base);   // (into scalar registers, also where the compiler does not see that it is uniform)
-    const uint64_t u = static_cast<uint32_t>(__builtin_amdgcn_readfirstlane(static_cast<int>(b))) |
-                       static_cast<uint64_t>(static_cast<uint32_t>(__builtin_amdgcn_readfirstlane(static_cast<int>(b >> 32)))) << 32;
-    asm volatile("s_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" :: "v"(byte_off), "s"(u), "{m0}"(lds) : "memory");
-}
 // Address = uniform base (kept in scalar registers) + unsigned 32-bit byte offset per lane: one add-free addressing
 // mode, no 64-bit vector arithmetic.
 __device__ __forceinline__ const void* at(const void* base, uint32_t byte_off) { return static_cast<const char*>(base) + byte_off; }

@@ -9,7 +9,7 @@
 namespace {
 
 // The kernels are built for gfx950 only; say so instead of failing inside the launch on another device.
-inline lordba_status check_device() {
+lordba_status check_device() {
     static std::mutex mu;
     static int state[64] = {0};  // 0 unknown, 1 ok, 2 not usable
     int dev = 0;

@@ -178,13 +178,13 @@ __global__ __launch_bounds__(64 * WC * WT * WK, 2) void lordba_i4_many_kernel(I4
         }
     };
     auto make = [&](auto depth, uint32_t buffer, const Weights& v) __attribute__((always_inline)) {
-        constexpr int d = depth.value, m = d >> 1, c = d & 1, set = d & 1;
+        constexpr int d = depth.value, m = d >> 1, c = d & 1, set = d & 1, early = A > 2 ? d % A : 0;
 #pragma unroll
         for (int i = 0; i < CP; ++i) {
             if constexpr (BWD) {
                 const int8_t* const at_s = lds + buffer + kX + s_at[i] + 32 * d + 16 * h;
-                const u4 s = A > 2 ? sv[d % A][i] : *reinterpret_cast<const u4*>(at_s);
-                if constexpr (ZERO) w[set][i] = operand(v.c[i][c][m], Zero8{A > 2 ? zv[d % A][i] : *reinterpret_cast<const u4*>(at_s + kS)}, exp);
+                const u4 s = A > 2 ? sv[early][i] : *reinterpret_cast<const u4*>(at_s);
+                if constexpr (ZERO) w[set][i] = operand(v.c[i][c][m], Zero8{A > 2 ? zv[early][i] : *reinterpret_cast<const u4*>(at_s + kS)}, exp);
                 else w[set][i] = operand(v.c[i][c][m], Zero1(kZero8), exp);
                 w[set][i] = w[set][i] * as_h8(s);
             } else {

@@ -27,6 +27,16 @@ struct I4Args {
 
 namespace {
 
+[[maybe_unused]] constexpr lordba_status (*kCheckDevice)() = check_device;   // (which the entry points alone call)
+
+// Sixteen bytes a lane into LDS, from a uniform base and a byte offset per lane.
+__device__ __forceinline__ void load16_to_lds_from(uint32_t lds, const void* base, uint32_t byte_off) {
+    const uint64_t b = reinterpret_cast<uint64_t>(base);   // (into scalar registers, also where the compiler does not see that it is uniform)
+    const uint64_t u = static_cast<uint32_t>(__builtin_amdgcn_readfirstlane(static_cast<int>(b))) |
+                       static_cast<uint64_t>(static_cast<uint32_t>(__builtin_amdgcn_readfirstlane(static_cast<int>(b >> 32)))) << 32;
+    asm volatile("s_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" :: "v"(byte_off), "s"(u), "{m0}"(lds) : "memory");
+}
+
 __device__ __forceinline__ h2 both(uint16_t v) { return as_h2(v * 0x10001u); }
 
 // The eight numbers code - zero of a word, exact in fp16.  With the biased exponent 0x64 a code in the low four bits of a half is 1024 + code, one four
