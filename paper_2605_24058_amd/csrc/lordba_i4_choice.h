@@ -10,18 +10,22 @@ namespace {
 
 // The tiles, and their times in microseconds: a step of `parts` blocks of 128 columns where the chip has room for more workgroups, the same as a share of a
 // full compute unit, and what comes around the steps of each round of workgroups.  (A step of the small tiles takes its microsecond for bringing the codes to fp16,
-// not for waiting: read two or three steps ahead it took as long.)  Fitted to some fifty shapes of 16 to 4000 tokens, 301 to 13001 columns and outputs, every
-// kernel timed on each.
-enum I4Kernel { kI4Few = 0, kI4Tile32 = 1, kI4Tile64 = 2, kI4Tile128 = 3, kI4Tile256 = 4 };
+// not for waiting: read two or three steps ahead it took as long.)  Fitted to every kernel's times on 318 calls of 9 to 2000 tokens, 512 to 11008 columns and 512 to
+// 32000 outputs, with and without zeros: there the pick is behind the best by 0.9 % in the mean and 19 % at worst.
+// The 64 x 64 tile brings each code to fp16 once where the 64 x 32 one does twice for 33 to 64 tokens, by eight waves of which each has half of the channels
+// (64 x 4096 -> 11008 19.1 -> 15.0 us, 33 x 5120 -> 13824 22.9 -> 19.8; on 15 of 117 forward shapes 3 to 25 % ahead of all others, never in the gradient: 36 against 23).
+enum I4Kernel { kI4Few = 0, kI4Tile32 = 1, kI4Tile64 = 2, kI4Tile128 = 3, kI4Tile256 = 4, kI4Square64 = 5 };
 struct I4Tile {
     int channels, tokens, parts, resident;   // resident: workgroups that a compute unit holds at a time
     double alone, share, fixed;
 };
-constexpr I4Tile kI4Tiles[5] = {{32, 16, 8, 2, 0.6, 1.65, 3.0},    // kernel for few tokens: the weights as they are, forward
-                                {32, 32, 8, 1, 1.2, 1.54, 2.0},    // (gated: 64 channels)
-                                {64, 32, 4, 2, 0.96, 0.87, 1.6},
-                                {128, 64, 2, 2, 1.05, 1.2, 1.0},
-                                {256, 128, 1, 2, 1.15, 1.87, 3.2}};
+constexpr I4Tile kI4Tiles[6] = {{32, 16, 8, 2, 1.1, 1.67, 2.17},     // kernel for few tokens: the weights as they are, forward
+                                {32, 32, 8, 1, 1.02, 1.44, 2.93},    // (gated: 64 channels)
+                                {64, 32, 4, 2, 0.94, 1.02, 2.7},
+                                {128, 64, 2, 2, 1.13, 1.3, 2.37},
+                                {256, 128, 1, 2, 1.46, 2.44, 3.09},
+                                {64, 64, 4, 1, 1.1, 1.43, 3.02}};    // forward, one matrix, aligned rows
+constexpr I4Tile kI4FewGradient = {32, 16, 8, 2, 1.5, 2.89, 1.0};    // (a scale and a zero for every code)
 // The same for rows that no request takes whole, which come through registers.
 constexpr I4Tile kI4Unaligned[5] = {{32, 16, 8, 2, 1.3, 2.4, 3.0}, {32, 32, 8, 1, 1.9, 2.9, 3.9}, {64, 32, 4, 2, 1.3, 1.0, 3.7}, {128, 64, 2, 2, 1.45, 1.48, 5.0},
                                     {256, 128, 1, 2, 1.6, 2.6, 3.0}};
@@ -37,12 +41,13 @@ inline double i4_cost(const I4Tile& t, int64_t channels, int64_t T, int64_t bloc
 }
 
 // T tokens, k columns of a plane of the contraction, `blocks` of 128 columns in all, n outputs; aligned: rows of whole 16-byte pieces
-inline I4Kernel i4_kernel(int64_t T, int64_t k, int64_t blocks, int64_t n, bool gated, bool aligned) {
+inline I4Kernel i4_kernel(int64_t T, int64_t k, int64_t blocks, int64_t n, bool gated, bool aligned, bool backward) {
     if (T <= kI4FewTokens || k < 8 || k > kI4MostColumns) return kI4Few;
     const int64_t channels = gated ? 2 * n : n;
     I4Kernel best = kI4Few;
-    double least = i4_cost((aligned ? kI4Tiles : kI4Unaligned)[0], channels, T, blocks);
-    for (int i = 1; i < 5; ++i) {
+    double least = i4_cost(!aligned ? kI4Unaligned[0] : backward ? kI4FewGradient : kI4Tiles[0], channels, T, blocks);
+    const int tiles = gated || backward || !aligned ? kI4Square64 : kI4Square64 + 1;
+    for (int i = 1; i < tiles; ++i) {
         I4Tile t = (aligned ? kI4Tiles : kI4Unaligned)[i];
         if (gated && i == kI4Tile32) t.channels = 64, t.share *= 2;
         const double cost = i4_cost(t, channels, T, blocks);

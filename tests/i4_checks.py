@@ -14,7 +14,7 @@ import numpy as np
 
 from paper_2605_24058_amd import binding
 
-KERNELS = ("few", "tile32", "tile64", "tile128", "tile256")
+KERNELS = ("few", "tile32", "tile64", "tile128", "tile256", "square64")    # (the last: forward, one matrix, aligned rows)
 # T, d_in, d_out (d_ff), group, zero points: one token and one column; ends of groups, of blocks of 128 columns, of 32 rows; both sides of the kernels' limits; odd
 # widths; rows that start anywhere; tiles of every size whole and with all sizes ragged; contractions of fewer blocks than a workgroup has parts and of many
 SHAPES = [(1, 1, 1, 32, True), (1, 128, 32, 128, False), (2, 31, 33, 32, True), (3, 127, 31, 64, False), (8, 129, 65, 128, True), (16, 256, 64, 64, True),
@@ -25,7 +25,8 @@ SHAPES = [(1, 1, 1, 32, True), (1, 128, 32, 128, False), (2, 31, 33, 32, True), 
           (32, 3328, 520, 128, True), (48, 2050, 1001, 64, False), (96, 2048, 1024, 32, True), (256, 1288, 4136, 128, False), (300, 1032, 1032, 32, True),
           (260, 5000, 264, 64, True), (640, 2056, 1536, 64, True), (1500, 520, 2056, 128, False), (1024, 1024, 4096, 32, False), (1100, 4104, 776, 128, True),
           (4100, 264, 520, 64, True), (2500, 1025, 700, 32, True), (40, 4104, 2072, 64, True), (64, 8192, 2048, 32, False), (60, 8200, 2051, 128, True),
-          (61, 8264, 1991, 64, False), (3, 300, 8300, 128, True), (8, 1030, 8321, 32, False), (1, 8400, 264, 64, True), (7, 8320, 130, 128, False)]
+          (61, 8264, 1991, 64, False), (3, 300, 8300, 128, True), (8, 1030, 8321, 32, False), (1, 8400, 264, 64, True), (7, 8320, 130, 128, False), (500, 1032, 2048, 32, False),
+          (63, 2056, 10001, 64, True), (130, 2112, 4096, 128, False)]
 
 
 @functools.lru_cache(None)
@@ -33,18 +34,18 @@ def _choice():
     """The choice of the kernel (csrc/lordba_i4_choice.h), compiled for the host."""
     with tempfile.TemporaryDirectory() as d:
         with open(os.path.join(d, "choice.cpp"), "w") as f:
-            f.write('#include "lordba_i4_choice.h"\nextern "C" int kernel(long long T, long long k, long long b, long long n, int g, int a) '
-                    "{ return i4_kernel(T, k, b, n, g != 0, a != 0); }\n")
+            f.write('#include "lordba_i4_choice.h"\nextern "C" int kernel(long long T, long long k, long long b, long long n, int g, int a, int w) '
+                    "{ return i4_kernel(T, k, b, n, g != 0, a != 0, w != 0); }\n")
         subprocess.run([os.environ.get("CXX", "g++"), "-O1", "-std=c++17", "-Wall", "-Wextra", "-Werror", "-fPIC", "-shared", "-I", binding._CSRC, f.name, "-o",
                         os.path.join(d, "choice.so")], check=True, capture_output=True, timeout=120)
         f = ctypes.CDLL(os.path.join(d, "choice.so")).kernel
-    f.restype, f.argtypes = ctypes.c_int, [ctypes.c_longlong] * 4 + [ctypes.c_int] * 2
+    f.restype, f.argtypes = ctypes.c_int, [ctypes.c_longlong] * 4 + [ctypes.c_int] * 3
     return f
 
 
-def kernel(T, columns, n, planes=1, gated=False, aligned=True):
+def kernel(T, columns, n, planes=1, gated=False, aligned=True, backward=False):
     """Which kernel contracts `planes` planes of `columns` columns with n outputs (gated: of each half)."""
-    return KERNELS[_choice()(T, columns, planes * -(-columns // 128), n, gated, aligned and columns % 8 == 0)]
+    return KERNELS[_choice()(T, columns, planes * -(-columns // 128), n, gated, aligned and columns % 8 == 0, backward)]
 
 
 def weights(torch, rng, rows, cols, group, zeros, tiny=False):
