@@ -13,7 +13,7 @@ namespace {
 // not for waiting: read two or three steps ahead it took as long.)  Fitted to every kernel's times on 318 calls of 9 to 2000 tokens, 512 to 11008 columns and 512 to
 // 32000 outputs, with and without zeros: there the pick is behind the best by 0.9 % in the mean and 19 % at worst.
 // The 64 x 64 tile brings each code to fp16 once where the 64 x 32 one does twice for 33 to 64 tokens, by eight waves of which each has half of the channels
-// (64 x 4096 -> 11008 19.1 -> 15.0 us, 33 x 5120 -> 13824 22.9 -> 19.8; on 15 of 117 forward shapes 3 to 25 % ahead of all others, never in the gradient: 36 against 23).
+// (64 x 4096 -> 11008 19 -> 15 us, 33 x 5120 -> 13824 22.9 -> 19.8; on 15 of 117 forward shapes 3 to 25 % ahead of all others, never in the gradient: 36 against 23).
 enum I4Kernel { kI4Few = 0, kI4Tile32 = 1, kI4Tile64 = 2, kI4Tile128 = 3, kI4Tile256 = 4, kI4Square64 = 5 };
 struct I4Tile {
     int channels, tokens, parts, resident;   // resident: workgroups that a compute unit holds at a time
