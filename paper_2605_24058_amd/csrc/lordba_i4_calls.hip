@@ -23,7 +23,7 @@ lordba_status product(I4Args a, const Weights& w, const I4Shape& s, int64_t grou
     a.shift = group == 32 ? 5 : group == 64 ? 6 : 7;
     a.aligned = a.k % 8 == 0 && !i8_misaligned(a.x, 16);
     const hipStream_t st = static_cast<hipStream_t>(stream);
-    const I4Kernel kernel = i4_kernel(a.T, a.k, a.blocks, a.n, gated, a.aligned != 0, backward);
+    const I4Kernel kernel = i4_kernel(a.T, a.k, a.blocks, a.n, gated, a.aligned != 0, backward, w.zero != nullptr && group == 32);
     return kernel == kI4Few ? lordba_i4_few(a, group, gated, backward, st) : lordba_i4_many(a, kernel, group, gated, backward, st);
 }
 

@@ -26,9 +26,11 @@ constexpr I4Tile kI4Tiles[6] = {{32, 16, 8, 2, 1.1, 1.67, 2.17},     // kernel f
                                 {256, 128, 1, 2, 1.46, 2.44, 3.09},
                                 {64, 64, 4, 1, 1.1, 1.43, 3.02}};    // forward, one matrix, aligned rows
 constexpr I4Tile kI4FewGradient = {32, 16, 8, 2, 1.5, 2.89, 1.0};    // (a scale and a zero for every code)
-// The same for rows that no request takes whole, which come through registers.
-constexpr I4Tile kI4Unaligned[5] = {{32, 16, 8, 2, 1.3, 2.4, 3.0}, {32, 32, 8, 1, 1.9, 2.9, 3.9}, {64, 32, 4, 2, 1.3, 1.0, 3.7}, {128, 64, 2, 2, 1.45, 1.48, 5.0},
-                                    {256, 128, 1, 2, 1.6, 2.6, 3.0}};
+// The same for rows that no request takes whole, which come through registers (219 calls, 0.5 % and 17 %).  The largest tile's registers do not hold those
+// as well as the scales and zeros of groups of 32 along a row (2000 x 11003 -> 4096 380 us, 128 x 64 tiles 284; without zeros 234 and 262).
+constexpr I4Tile kI4Unaligned[5] = {{32, 16, 8, 2, 0.24, 3.27, 2.92}, {32, 32, 8, 1, 2.02, 2.14, 5.23}, {64, 32, 4, 2, 1.47, 1.65, 3.57}, {128, 64, 2, 2, 1.74, 1.55, 4.75},
+                                    {256, 128, 1, 2, 2.11, 3.0, 4.73}};
+constexpr I4Tile kI4UnalignedFewGradient = {32, 16, 8, 2, 0.84, 4.2, 3.44};
 constexpr double kI4Launch = 2.5;
 
 constexpr int64_t kI4MostColumns = 1 << 22;   // of a plane: a tile's rows span less than 4 GiB
@@ -40,14 +42,15 @@ inline double i4_cost(const I4Tile& t, int64_t channels, int64_t T, int64_t bloc
     return kI4Launch + t.fixed * rounds + steps * std::max(t.alone * rounds, n / 256 * t.share);
 }
 
-// T tokens, k columns of a plane of the contraction, `blocks` of 128 columns in all, n outputs; aligned: rows of whole 16-byte pieces
-inline I4Kernel i4_kernel(int64_t T, int64_t k, int64_t blocks, int64_t n, bool gated, bool aligned, bool backward) {
+// T tokens, k columns of a plane of the contraction, `blocks` of 128 columns in all, n outputs; aligned: rows of whole 16-byte pieces; fine_zeros: zeros, groups of 32
+inline I4Kernel i4_kernel(int64_t T, int64_t k, int64_t blocks, int64_t n, bool gated, bool aligned, bool backward, bool fine_zeros) {
     if (T <= kI4FewTokens || k < 8 || k > kI4MostColumns) return kI4Few;
     const int64_t channels = gated ? 2 * n : n;
     I4Kernel best = kI4Few;
-    double least = i4_cost(!aligned ? kI4Unaligned[0] : backward ? kI4FewGradient : kI4Tiles[0], channels, T, blocks);
+    double least = i4_cost(backward ? (aligned ? kI4FewGradient : kI4UnalignedFewGradient) : (aligned ? kI4Tiles : kI4Unaligned)[kI4Few], channels, T, blocks);
     const int tiles = gated || backward || !aligned ? kI4Square64 : kI4Square64 + 1;
     for (int i = 1; i < tiles; ++i) {
+        if (i == kI4Tile256 && !aligned && !backward && fine_zeros) continue;
         I4Tile t = (aligned ? kI4Tiles : kI4Unaligned)[i];
         if (gated && i == kI4Tile32) t.channels = 64, t.share *= 2;
         const double cost = i4_cost(t, channels, T, blocks);

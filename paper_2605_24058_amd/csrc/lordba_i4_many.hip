@@ -430,8 +430,10 @@ lordba_status many(const I4Args& a, int kernel, hipStream_t stream) {
     if (!a.aligned) {
         if (kernel == kI4Tile32) return many_launch<GATED ? 2 : 1, 1, 1, 1, 8, S, ZERO, GATED, true>(a, stream);
         if (kernel == kI4Tile64) return many_launch<2, 1, 1, 1, 4, S, ZERO, GATED, true>(a, stream);
-        if (kernel == kI4Tile128) return many_launch<2, 2, 2, 1, 2, S, ZERO, GATED, true>(a, stream);
-        return many_launch<2, 4, 4, 1, 1, S, ZERO, GATED, true>(a, stream);
+        if constexpr (!(S == 4 && ZERO)) {
+            if (kernel == kI4Tile256) return many_launch<2, 4, 4, 1, 1, S, ZERO, GATED, true>(a, stream);
+        }
+        return many_launch<2, 2, 2, 1, 2, S, ZERO, GATED, true>(a, stream);
     }
     if constexpr (S > 0 && !GATED) {
         if (kernel == kI4Square64) return many_launch<1, 2, 2, 1, 4, S, ZERO, GATED, false>(a, stream);

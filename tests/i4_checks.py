@@ -34,18 +34,18 @@ def _choice():
     """The choice of the kernel (csrc/lordba_i4_choice.h), compiled for the host."""
     with tempfile.TemporaryDirectory() as d:
         with open(os.path.join(d, "choice.cpp"), "w") as f:
-            f.write('#include "lordba_i4_choice.h"\nextern "C" int kernel(long long T, long long k, long long b, long long n, int g, int a, int w) '
-                    "{ return i4_kernel(T, k, b, n, g != 0, a != 0, w != 0); }\n")
+            f.write('#include "lordba_i4_choice.h"\nextern "C" int kernel(long long T, long long k, long long b, long long n, int g, int a, int w, int f) '
+                    "{ return i4_kernel(T, k, b, n, g != 0, a != 0, w != 0, f != 0); }\n")
         subprocess.run([os.environ.get("CXX", "g++"), "-O1", "-std=c++17", "-Wall", "-Wextra", "-Werror", "-fPIC", "-shared", "-I", binding._CSRC, f.name, "-o",
                         os.path.join(d, "choice.so")], check=True, capture_output=True, timeout=120)
         f = ctypes.CDLL(os.path.join(d, "choice.so")).kernel
-    f.restype, f.argtypes = ctypes.c_int, [ctypes.c_longlong] * 4 + [ctypes.c_int] * 3
+    f.restype, f.argtypes = ctypes.c_int, [ctypes.c_longlong] * 4 + [ctypes.c_int] * 4
     return f
 
 
-def kernel(T, columns, n, planes=1, gated=False, aligned=True, backward=False):
+def kernel(T, columns, n, planes=1, gated=False, aligned=True, backward=False, fine_zeros=False):
     """Which kernel contracts `planes` planes of `columns` columns with n outputs (gated: of each half)."""
-    return KERNELS[_choice()(T, columns, planes * -(-columns // 128), n, gated, aligned and columns % 8 == 0, backward)]
+    return KERNELS[_choice()(T, columns, planes * -(-columns // 128), n, gated, aligned and columns % 8 == 0, backward, fine_zeros)]
 
 
 def weights(torch, rng, rows, cols, group, zeros, tiny=False):

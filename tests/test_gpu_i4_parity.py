@@ -40,7 +40,7 @@ def test_linear_and_gradient(torch, T, d_in, d_out, group, zeros, shift):
     codes, scale, zero = i4_checks.weights(torch, rng, d_out, d_in, group, zeros)
     x, g = mem.input(acts(torch, rng, T, d_in), shift), mem.input(acts(torch, rng, T, d_out), shift)
     for backward in (False, True):
-        W = i4_checks.real(torch, codes, scale, zero, group, rounded=backward or i4_checks.kernel(T, d_in, d_out, aligned=shift == 0) != "few").cuda()
+        W = i4_checks.real(torch, codes, scale, zero, group, rounded=backward or i4_checks.kernel(T, d_in, d_out, aligned=shift == 0, fine_zeros=zeros and group == 32) != "few").cuda()
         y = mem.output((T, d_in if backward else d_out), torch.float16, shift)
         i8_checks.call(torch, "lordba_linear_i4" + "_backward" * backward, g if backward else x, *laid_out(torch, mem, codes, scale, zero, group, 1, backward), y,
                        T, d_in, d_out, group)
@@ -56,7 +56,7 @@ def test_gated_and_gradient(torch, T, d_in, d_ff, group, zeros, shift):
     mem = i8_checks.Memory(torch)
     codes, scale, zero = i4_checks.weights(torch, rng, 2 * d_ff, d_in, group, zeros)
     x, add, dh = mem.input(acts(torch, rng, T, d_in), shift), mem.input(torch.randn(2, T, d_ff).half().cuda(), shift), mem.input(acts(torch, rng, T, d_ff), shift)
-    W = i4_checks.real(torch, codes, scale, zero, group, rounded=i4_checks.kernel(T, d_in, d_ff, gated=True, aligned=shift == 0) != "few").cuda()
+    W = i4_checks.real(torch, codes, scale, zero, group, rounded=i4_checks.kernel(T, d_in, d_ff, gated=True, aligned=shift == 0, fine_zeros=zeros and group == 32) != "few").cuda()
     L = laid_out(torch, mem, codes, scale, zero, group, 2)
     both, err = i4_checks.product(torch, x.double(), W)
     for addends, keep in ((add, True), (None, False)):
