@@ -53,6 +53,15 @@ __host__ __device__ constexpr int64_t i4_row(int64_t t, int r) { return 32 * (t 
 
 constexpr uint16_t kZero8 = 0x6408;   // 1024 + 8 in fp16
 
+// dgate and dup of the gated block, before they are rounded
+__device__ __forceinline__ void slopes(float d, float gate, float up, float& dg, float& du) {
+    // silu' = sigma (1 + gate (1 - sigma)) with 1 - sigma = e / (1 + e): no cancellation where sigma is near 1
+    const float e = __expf(-fabsf(gate)), r = __builtin_amdgcn_rcpf(1.f + e);
+    const float sigma = gate < 0.f ? e * r : r, rest = gate < 0.f ? r : e * r;
+    dg = d * up * sigma * (1.f + gate * rest);
+    du = d * gate * sigma;
+}
+
 }  // namespace
 
 // dgate and dup of the gated block in fp16, [2, T, d_ff]

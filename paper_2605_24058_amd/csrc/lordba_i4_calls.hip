@@ -98,6 +98,7 @@ extern "C" lordba_status lordba_gated_i4_backward(const void* dh, const void* ga
     if ((st = lordba_i4_gated_grad(dh, gate_up, dgate_up, T, d_ff, static_cast<hipStream_t>(stream))) != LORDBA_OK) return st;
     I4Args a = {};
     a.x = static_cast<const _Float16*>(dgate_up), a.y = static_cast<_Float16*>(dx);
+    a.dh = static_cast<const _Float16*>(dh), a.gate_up = static_cast<const _Float16*>(gate_up);
     a.T = T, a.k = d_ff, a.n = d_in;
     return product(a, w, s, group, false, true, stream);
 }

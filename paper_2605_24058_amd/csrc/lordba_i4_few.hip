@@ -197,6 +197,9 @@ __global__ __launch_bounds__(64 * NW, NW <= 8 ? 4 : 1) void lordba_i4_few_kernel
                 a.y[to] = static_cast<_Float16>(v[0][e]);
             }
         }
+        if constexpr (BWD) {
+            if (a.dh && !number(v[0][0])) from_unrounded<4>(a, t, c);
+        }
     }
 }
 

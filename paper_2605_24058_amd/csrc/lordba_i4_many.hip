@@ -309,6 +309,7 @@ __global__ __launch_bounds__(64 * WC * WT * WK, 2) void lordba_i4_many_kernel(I4
 
     // Results of a block, of both halves where there are two: a lane has two times eight consecutive columns of a token.
     const int64_t plane = a.T * a.n;
+    uint32_t lost = 0;   // backward: blocks whose first result of this lane's is no number, bit i TB + j
     auto finish = [&](auto whole, auto odd, int i, int j, const sums16 (&sum)[P]) __attribute__((always_inline)) {
         constexpr bool FULL = whole.value, ODD = odd.value;
         const int64_t t = first_token + (wt * TB + j) * 32 + n;
@@ -342,6 +343,7 @@ __global__ __launch_bounds__(64 * WC * WT * WK, 2) void lordba_i4_many_kernel(I4
             }
             if constexpr (ODD) store8_odd<false, 32>(a.y + t * a.n + c, v[0]);
             else store8<FULL, false, false>(a.y + t * a.n, c, a.n, v[0]);
+            if (BWD && u == 0) lost |= number(v[0][0]) ? 0u : 1u << (i * TB + j);
         }
     };
     const bool full = 32 * static_cast<int64_t>(first_pair + kPairs) <= a.n && first_token + kTokens <= a.T;
@@ -389,6 +391,17 @@ __global__ __launch_bounds__(64 * WC * WT * WK, 2) void lordba_i4_many_kernel(I4
             if (!full) finish(std::false_type{}, std::false_type{}, i, j, sum);
             else if (odd) finish(std::true_type{}, std::true_type{}, i, j, sum);
             else finish(std::true_type{}, std::false_type{}, i, j, sum);
+        }
+    }
+    if constexpr (BWD) {
+        if (a.dh && lost) {
+            asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // (where every other row starts in the middle of a word, another lane has stored them)
+            const int me = __builtin_amdgcn_mbcnt_hi(~0u, __builtin_amdgcn_mbcnt_lo(~0u, 0u));   // (the lane once more: kept from the start it takes a register of the largest tile that is not there)
+            for (; lost; lost &= lost - 1) {
+                const int o = __builtin_ctz(lost);
+                for (int u = 0; u < 2; ++u)
+                    from_unrounded<8>(a, first_token + (wt * TB + o % TB) * 32 + (me & 31), 32 * static_cast<int64_t>(pair0 + o / TB) + 16 * u + 8 * (me >> 5));
+            }
         }
     }
 }

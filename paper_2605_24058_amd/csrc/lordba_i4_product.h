@@ -15,6 +15,7 @@ struct I4Args {
     const _Float16* addends;   // gated: [2, T, n], or null
     _Float16* y;               // [T, n]
     _Float16* kept;            // gated: [2, T, n], or null
+    const _Float16 *dh, *gate_up;   // the gated block's gradient: what x was made of, [T, k] and [2, T, k]; otherwise null
     int64_t T, k, n;
     int32_t blocks, plane_blocks;   // of 128 columns: in all, of a plane
     int32_t tiles;             // blocks of 16 rows of a half
@@ -71,6 +72,62 @@ __device__ __forceinline__ f4 mfma(h8 a, h8 b, f4 c) { return __builtin_amdgcn_m
 
 // For the backward pass: what passes the range of fp16 is kept as its largest number, a NaN as one.
 __device__ __forceinline__ _Float16 kept_half(float v) { return static_cast<_Float16>(v != v ? v : fminf(fmaxf(v, -65504.f), 65504.f)); }
+
+// The gated block's gradient at columns c .. c + N - 1 (c a multiple of N) of token t once more, of dgate and dup before they are rounded to fp16: where one of
+// them passes its range, the product has an infinity times every weight, those that are 0 among them, in place of a number, in all of the token's columns.
+// One lane alone, in fp32 (weights unrounded), a block of 128 columns by itself so that sums stay short.  What is no number by itself is left as the product gave it.
+// 2048 tokens of 4096 <- 2 x 11008, all of them past the range: 54 ms (in range the call takes 0.39, and as long as without the question).
+__device__ __forceinline__ bool number(float v) { return fabsf(v) < __builtin_inff(); }
+template <int N>
+__device__ __forceinline__ void from_unrounded(const I4Args& a, int64_t t, int64_t c) {
+    if (c >= a.n) return;
+    const int row = static_cast<int>(c & 31), in = 4 * (row >> 3) + (row & 3);   // c's place in a pair of blocks: i4_row() the other way round
+    const int64_t tile = 2 * (c >> 5) + (row >> 2 & 1), scales = (c >> a.shift) * a.blocks * kI4Columns;
+    const uint32_t* const codes = reinterpret_cast<const uint32_t*>(a.codes);
+    float sum[N];
+#pragma unroll
+    for (int e = 0; e < N; ++e) sum[e] = 0.f;
+    for (int b = 0; b < a.blocks; ++b) {
+        const int half = b >= a.plane_blocks;
+        const int64_t j0 = static_cast<int64_t>(b - half * a.plane_blocks) * kI4Columns;
+        const _Float16 *const d = a.dh + t * a.k, *const g = a.gate_up + t * a.k, *const u = g + a.T * a.k;
+        float part[N];
+#pragma unroll
+        for (int e = 0; e < N; ++e) part[e] = 0.f;
+        for (int w = 0; w < 16 && j0 + 8 * w < a.k; ++w) {
+            const h8 hd = as_h8(load_part(d, j0 + 8 * w, a.k)), hg = as_h8(load_part(g, j0 + 8 * w, a.k)), hu = as_h8(load_part(u, j0 + 8 * w, a.k));
+            const int64_t at = scales + static_cast<int64_t>(b) * kI4Columns + 8 * w;
+            const h8 s = as_h8(load16(a.scale + at));
+            const u4 z = a.zero ? load16(a.zero + at) : u4{kZero8 * 0x10001u, kZero8 * 0x10001u, kZero8 * 0x10001u, kZero8 * 0x10001u};
+            float v[8];
+            bool numbers = true;
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+                float dg, du;
+                slopes(static_cast<float>(hd[k]), static_cast<float>(hg[k]), static_cast<float>(hu[k]), dg, du);
+                v[k] = half ? du : dg;
+                v[k] *= static_cast<float>(s[k]);
+                numbers = numbers && number(v[k]);
+            }
+            if (!numbers) return;
+#pragma unroll
+            for (int e = 0; e < N; ++e) {
+                const int at_row = in + (e & 3);
+                const uint32_t code = codes[(((tile + (e >> 2)) * a.blocks + b) * 64 + 16 * (w & 3) + at_row) * 4 + (w >> 2)];
+#pragma unroll
+                for (int k = 0; k < 8; ++k) {
+                    const int zero = z[k >> 1] >> (16 * (k & 1)) & 15;
+                    part[e] = fmaf(v[k], static_cast<float>(static_cast<int>(code >> (4 * i4_nibble(k)) & 15) - zero), part[e]);
+                }
+            }
+        }
+#pragma unroll
+        for (int e = 0; e < N; ++e) sum[e] += part[e];
+    }
+#pragma unroll
+    for (int e = 0; e < N; ++e)
+        if (c + e < a.n) a.y[t * a.n + c + e] = static_cast<_Float16>(sum[e]);
+}
 
 __device__ __forceinline__ float silu(float v) { return v * __builtin_amdgcn_rcpf(1.f + __expf(-v)); }
 

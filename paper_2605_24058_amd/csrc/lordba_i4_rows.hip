@@ -134,14 +134,6 @@ struct GatedGradArgs {
     int64_t n;   // elements of a plane
 };
 
-__device__ __forceinline__ void slopes(float d, float gate, float up, float& dg, float& du) {
-    // silu' = sigma (1 + gate (1 - sigma)) with 1 - sigma = e / (1 + e): no cancellation where sigma is near 1
-    const float e = __expf(-fabsf(gate)), r = __builtin_amdgcn_rcpf(1.f + e);
-    const float sigma = gate < 0.f ? e * r : r, rest = gate < 0.f ? r : e * r;
-    dg = d * up * sigma * (1.f + gate * rest);
-    du = d * gate * sigma;
-}
-
 __global__ __launch_bounds__(256) void lordba_i4_gated_grad_kernel(GatedGradArgs a) {
     const int64_t stride = static_cast<int64_t>(gridDim.x) * 256 * 8;
     for (int64_t k = (static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x) * 8; k < a.n; k += stride) {
