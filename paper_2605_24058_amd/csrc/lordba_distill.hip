@@ -104,12 +104,12 @@ constexpr int kInWave = 64;   // entries up to which the first wave compares the
 template <class E, int THREADS, int NV, bool TWO>
 __global__ __launch_bounds__(THREADS) void lordba_distill_kernel(DistillArgs a) {
     constexpr int N = Pack<E>::N, W = THREADS / 64;
-    __shared__ float partial[3][W], teacher[2];   // largest, sums of the waves; the teacher's largest logit and log of its sum
+    __shared__ float partial[3][W], teacher[2];   // largest, sums of the waves; the teacher's largest logit and its sum
     __shared__ int32_t some;                      // whether the teacher has an entry
-    extern __shared__ int32_t index[];            // [k + 1], the label last; then, as many each:
-    float* const p = reinterpret_cast<float*>(index + a.k + 1);   // the teacher's probability,
-    float* const at = p + a.k + 1;                                // the student's logit,
-    float* const off = at + a.k + 1;                              // what the entry takes off, of all that name the same one; below 0 where another one stands for it
+    extern __shared__ int32_t index[];            // [k]; then, as many each:
+    float* const p = reinterpret_cast<float*>(index + a.k);   // the teacher's logit,
+    float* const off = p + a.k;                               // what the entry takes off, of all that name the same one; below 0 where another one stands for it;
+    float* const at = off + a.k;                              // the student's logit, and behind the last the label's
     const int64_t t = a.first + blockIdx.x, V = a.V;
     const E* const z = static_cast<const E*>(a.z) + t * V;
     E* const grad = a.grad ? static_cast<E*>(a.grad) + t * V : nullptr;
@@ -173,7 +173,6 @@ __global__ __launch_bounds__(THREADS) void lordba_distill_kernel(DistillArgs a) 
         }
         if (lane == 0) {
             teacher[0] = most, teacher[1] = total;
-            index[a.k] = has_hard ? label : -1;
             at[a.k] = has_hard ? static_cast<float>(z[label]) : 0.f;
         }
         const bool any = __any(mine);
@@ -309,7 +308,7 @@ template <class E, int THREADS, int NV, bool TWO>
 lordba_status distill_launch(DistillArgs a, int64_t T, hipStream_t stream) {
     constexpr int64_t kMost = (static_cast<int64_t>(1) << 31) / THREADS / 2;   // (a launch counts threads in 32 bits)
     for (a.first = 0; a.first < T; a.first += kMost) {
-        hipLaunchKernelGGL((lordba_distill_kernel<E, THREADS, NV, TWO>), dim3(static_cast<unsigned>(std::min(kMost, T - a.first))), dim3(THREADS), static_cast<size_t>(a.k + 1) * 16, stream, a);
+        hipLaunchKernelGGL((lordba_distill_kernel<E, THREADS, NV, TWO>), dim3(static_cast<unsigned>(std::min(kMost, T - a.first))), dim3(THREADS), static_cast<size_t>(a.k) * 16 + 4, stream, a);
         const lordba_status st = i8_launched();
         if (st != LORDBA_OK) return st;
     }
