@@ -567,7 +567,7 @@ typedef struct {
     const void* top_logits;    /* [T, k], of the logits' type                                  */
     const int32_t* labels;     /* [T], or NULL: none                                           */
     int64_t k;                 /* 0 .. LORDBA_MAX_TOP                                          */
-    float temperature;         /* > 0                                                          */
+    float temperature;         /* > 0, a normal number                                         */
     float soft, hard;          /* factors of the two terms, finite                             */
 } lordba_teacher;
 #define LORDBA_MAX_TOP 1024

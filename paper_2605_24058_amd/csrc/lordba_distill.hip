@@ -246,11 +246,12 @@ __global__ __launch_bounds__(THREADS) void lordba_distill_kernel(DistillArgs a) 
         for (int i = lane; i < a.k; i += 64)
             if (index[i] >= 0) {
                 const float arg = p[i] - teacher[0], pr = __builtin_amdgcn_exp2f(arg * cu) / teacher[1];
-                if (pr != 0.f) part += pr * ((arg / a.u - log_total) - ((at[i] - m) / a.u - log_s));
+                // u times the difference of the logarithms, without a quotient that small temperatures would take past the range
+                if (pr != 0.f) part += pr * ((arg - (at[i] - m)) + a.u * (log_s - log_total));
             }
         part = wave_sum(part);
         if (lane == 0) {
-            float loss = has_soft ? a.soft * a.u * a.u * part : 0.f;
+            float loss = has_soft ? a.soft * a.u * part : 0.f;
             if (has_hard) loss -= a.hard * ((at[a.k] - m) - logf(s1));
             a.loss[t] = loss;
             const bool none = !has_soft && !has_hard;
@@ -339,7 +340,7 @@ lordba_status run(const void* logits, int type, const lordba_teacher* w, const f
     if (T < 0 || T > INT32_MAX || V < 1 || V > (1 << 24)) return LORDBA_ERR_DIM;
     if (!w) return LORDBA_ERR_NULL;
     if (w->k < 0 || w->k > LORDBA_MAX_TOP) return LORDBA_ERR_DIM;
-    if ((type != LORDBA_F16 && type != LORDBA_F32) || !(w->temperature > 0.f) || !std::isfinite(w->temperature) || !std::isfinite(w->soft) ||
+    if ((type != LORDBA_F16 && type != LORDBA_F32) || !(w->temperature > 0.f) || !std::isnormal(w->temperature) || !std::isfinite(w->soft) ||
         !std::isfinite(w->hard))
         return LORDBA_ERR_VALUE;
     if (T == 0) return LORDBA_OK;
