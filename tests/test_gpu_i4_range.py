@@ -1,4 +1,4 @@
-"""The gated block on 4-bit weights where its gradients with respect to gate and up pass the range of fp16: the input's gradient is a number for many of them, and has to be that number."""
+"""The gated block on 4-bit weights where gate, up and the gradients with respect to them pass the range of fp16: what comes of them is a number for many, and has to be that number."""
 import numpy as np
 import pytest
 
@@ -79,3 +79,53 @@ def test_what_is_no_number_stays_in_its_token(torch, T, d_in, F, group, zeros, k
     others[0] = others[T - 1] = False
     assert torch.equal(dx2[others], dx[others]) and torch.equal(dgu2[:, others], dgu[:, others])
     assert not bool(torch.isfinite(dx2[0]).any()) and bool(torch.isnan(dx2[T - 1]).all())
+
+
+@pytest.mark.parametrize("shift", [0, 1], ids=["aligned", "by-one"])
+@pytest.mark.parametrize("T,d_in,F,group,kernel", [(2, 2, 40, 32, "few"), (5, 40, 41, 64, "few"), (40, 528, 1501, 128, "tile32"), (17, 264, 1991, 32, "tile64"), (17, 40, 1991, 64, "tile128"),
+                                                   (200, 40, 8200, 128, "tile256"), (200, 40, 8199, 32, "tile256")])
+def test_a_gate_past_the_range_has_finite_gradients(torch, T, d_in, F, group, kernel, shift):
+    # x = (600, 0, ...): one weight of 15 x 8 gives +-72000; gate and up get the rest from the addends, and silu(-12) = -7.4e-5, so their product with 72000 is small
+    assert shift or i4_checks.kernel(T, d_in, F, gated=True) == kernel
+    rng, kind = np.random.default_rng(F), np.arange(F) % 5
+    sign = np.concatenate([np.choose(kind, [-1, 1, 0, 0, -1]), np.choose(kind, [0, 0, 1, -1, 0])])
+    zero = np.where(sign < 0, 15, np.where(sign > 0, 0, 6)).astype(np.uint8)[:, None].repeat(-(-d_in // group), axis=1)
+    codes = np.repeat(zero[:, :1], d_in, axis=1)
+    codes[:, 0] = np.where(sign < 0, 0, np.where(sign > 0, 15, 6))
+    x = np.zeros((T, d_in), np.float16)
+    x[:, 0] = 600
+    add = rng.uniform(0.001, 0.01, size=(2, T, F)).astype(np.float16)
+    add[0][:, kind >= 2] -= np.float16(12)
+    cu = lambda a: torch.from_numpy(a).cuda()
+    plain = cu(codes), torch.full(zero.shape, 8.0, dtype=torch.float16, device="cuda"), cu(zero)
+    mem = i8_checks.Memory(torch)
+    h, kept = mem.output((T, F), torch.float16, shift), mem.output((2, T, F), torch.float16, shift)
+    laid = binding.lordba_layout_i4(*plain, group, halves=2)
+    i8_checks.call(torch, "lordba_gated_i4", mem.input(x, shift), laid.codes, laid.scale, laid.zero, mem.input(add, shift), h, kept, T, d_in, F, group)
+    mem.unchanged()
+    base = cu(600.0 * 120.0 * sign)
+    gate, up = base[:F] + cu(add[0]).double(), base[F:] + cu(add[1]).double()
+    silu = gate * torch.sigmoid(gate)
+    assert float(gate.abs().max()) > 70000 < float(up.abs().max()) and float((silu * up).abs().max()) < 1000
+    # (the product is exact; the addition is rounded)
+    eg, eu = gate.abs() * 2.0 ** -24, up.abs() * 2.0 ** -24
+    i8_checks.near(h, silu * up, 1.1 * up.abs() * eg + silu.abs() * eu + (silu * up).abs() * 2.0 ** -18 * (1 + gate.abs() / 16))
+    i8_checks.near(kept[0], gate.clamp(-LARGEST, LARGEST), eg)
+    i8_checks.near(kept[1], up.clamp(-LARGEST, LARGEST), eu)
+    dh = rng.uniform(0.1, 0.5, size=(T, F)).astype(np.float16)
+    dx, dgu = binding.lordba_gated_i4_backward(cu(dh), kept, binding.lordba_layout_i4(*plain, group, halves=2, transposed=True))
+    dg, du, eg, eu = i8_checks.gated_gradient(torch, dh, kept.cpu().numpy())
+    i8_checks.near(dgu[0], dg, eg)
+    i8_checks.near(dgu[1], du, eu)
+    assert bool(torch.isfinite(dgu).all()) and not bool(torch.isnan(dx).any())
+
+
+def test_what_is_no_number_is_kept_as_none(torch):
+    for T, F in ((4, 70), (40, 70), (200, 1000)):
+        add = np.zeros((2, T, F), np.float16)
+        add[0, 3, 5], add[1, T // 2, 69], add[0, 1, 7], add[1, T - 1, 0] = np.nan, np.nan, np.inf, -np.inf
+        W = binding.lordba_layout_i4(torch.full((2 * F, 9), 8, dtype=torch.uint8, device="cuda"), torch.ones(2 * F, 1, dtype=torch.float16, device="cuda"), group=32, halves=2)
+        h, kept = binding.lordba_gated_i4(torch.ones(T, 9, dtype=torch.float16, device="cuda"), W, addends=torch.from_numpy(add).cuda(), save=True)
+        want = np.where(np.isinf(add), np.sign(add) * LARGEST, add.astype(np.float64))
+        assert np.array_equal(kept.cpu().numpy().astype(np.float64), want, equal_nan=True)
+        assert np.isnan(h.cpu().numpy()[[3, T // 2, 1], [5, 69, 7]]).all()     # (infinity times an up of 0)
