@@ -516,6 +516,7 @@ size_t lordba_i4_scale_count(int64_t rows, int64_t cols, int64_t group, int halv
  * each [rows, ceil(cols / group)], or NULL for symmetric codes:
  *     symmetric: scale = fp16(amax / 7), zero = 8;   with zeros: scale = fp16((high - low) / 15), zero = rint(-low / scale) to 15 at most, where low <= 0 <= high
  *     code = rint(w / scale + zero) between 0 and 15                                                          (fp32; ties to even)
+ * A weight within a step (a scale) of the end of the range of fp16 may get a code that stands for a number past it, which the products then take as an infinity (see above).
  * A group whose scale is 0 gets codes that stand for 0; one that holds an infinity or a NaN the scale NaN.  group other than 32, 64, 128 -> LORDBA_ERR_VALUE. */
 lordba_status lordba_quantize_i4(const void* w, uint8_t* codes, void* scale, uint8_t* zero, int64_t rows, int64_t cols, int64_t group, void* stream);
 

@@ -28,6 +28,7 @@ constexpr I4Tile kI4Tiles[6] = {{32, 16, 8, 2, 1.1, 1.67, 2.17},     // kernel f
 constexpr I4Tile kI4FewGradient = {32, 16, 8, 2, 1.5, 2.89, 1.0};    // (a scale and a zero for every code)
 // The same for rows that no request takes whole, which come through registers (219 calls, 0.5 % and 17 %).  The largest tile's registers do not hold those
 // as well as the scales and zeros of groups of 32 along a row (2000 x 11003 -> 4096 380 us, 128 x 64 tiles 284; without zeros 234 and 262).
+// Eleven of the largest tile's other forms keep 1 to 16 registers in memory, the aligned ones of groups of 32 with zeros among them, and are counted like the rest.
 constexpr I4Tile kI4Unaligned[5] = {{32, 16, 8, 2, 0.24, 3.27, 2.92}, {32, 32, 8, 1, 2.02, 2.14, 5.23}, {64, 32, 4, 2, 1.47, 1.65, 3.57}, {128, 64, 2, 2, 1.74, 1.55, 4.75},
                                     {256, 128, 1, 2, 2.11, 3.0, 4.73}};
 constexpr I4Tile kI4UnalignedFewGradient = {32, 16, 8, 2, 0.84, 4.2, 3.44};

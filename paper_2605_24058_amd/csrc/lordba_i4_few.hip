@@ -233,6 +233,8 @@ lordba_status few(const I4Args& a, hipStream_t stream) {
     // 13001 -> 301 6.7, with eight 7.1, with four 9.0), but backward, where a wave's scales take as many registers as its codes, eight (16 x 4096 -> 4096 8.8,
     // with sixteen 10.6).  Between them, and with more tokens, whose staging then is the larger part, eight waves, on two blocks of rows (16 x 4096 -> 11008 18.5 ->
     // 14.8 us).
+    // Not all forms have room for their ring in the 128 registers that sixteen waves on a compute unit leave each: gated with groups of 64 and zeros 47 lie in memory, without 12, with zeros and groups of 32
+    // or 128 11 and 8, of the gradient on two blocks of rows with zeros 33, of the forward product there with zeros and groups of 32 11.  Shallower rings for these have not been measured.
     constexpr int P = GATED ? 2 : 1, D = S == 0 || S == 4 ? 2 : 4;
     if (a.tiles > 512 && a.T <= 8) return few_launch<P, 4, D, S, ZERO, GATED>(a, stream);
     if constexpr (S > 0 && !GATED) {

@@ -29,7 +29,8 @@ typedef float sums16 __attribute__((ext_vector_type(16)));
 // Weights.  They come from memory straight into the registers of the waves that multiply them, a step ahead.  A pair of 16-row blocks is a 32-row operand: lane
 // 32 h + 16 b + r takes from block b what lanes 16 (2 c + h) + r hold (lordba_i4.h), which is row r's columns 32 m + 16 c + 8 h .. + 7 for m = 0 .. 3 and c = 0, 1.
 // They become fp16 in the registers, their scale multiplied on before the product, which rounds each weight once (half a step, 2^-11 of it; scales taken out of
-// the sums instead, as for few tokens, would be exact, but take a multiplication for every accumulator and group).
+// the sums instead, as for few tokens, would be exact, but take a multiplication for every accumulator and group: 64 against 32 for a 32 x 128 block of weights in the
+// largest tile at groups of 128, whose registers do not hold a second set of accumulators besides.  In tiles of 32 tokens it would be 16 against 32, which has not been measured).
 // While the products of one depth run, the operands of the next are read from LDS and made from the codes.  The barrier stands one depth before a step's
 // end: everybody has then read the step's activations, and the next step's have landed.
 template <int CP, int TB, int WC, int WT, int WK, int S, bool ZERO, bool GATED, bool BY_REGISTERS>
