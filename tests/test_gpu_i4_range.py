@@ -129,3 +129,28 @@ def test_what_is_no_number_is_kept_as_none(torch):
         want = np.where(np.isinf(add), np.sign(add) * LARGEST, add.astype(np.float64))
         assert np.array_equal(kept.cpu().numpy().astype(np.float64), want, equal_nan=True)
         assert np.isnan(h.cpu().numpy()[[3, T // 2, 1], [5, 69, 7]]).all()     # (infinity times an up of 0)
+
+
+@pytest.mark.parametrize("T,d_in,F,group,zeros,kernel", CASES[1::4])
+def test_gradients_past_the_range_in_graphs_and_on_two_streams(torch, T, d_in, F, group, zeros, kernel):
+    codes, scale, zero, dh, gate_up = inputs(torch, T, d_in, F, group, zeros)
+    laid = binding.lordba_layout_i4(codes.cuda(), scale.cuda(), None if zero is None else zero.cuda(), group, halves=2, transposed=True)
+    d, gu = torch.from_numpy(dh).cuda(), torch.from_numpy(gate_up).cuda()
+    call = lambda **kw: binding.lordba_gated_i4_backward(d, gu, laid, **kw)
+    want = [t.clone() for t in call()]
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    for s in streams:
+        s.wait_stream(torch.cuda.current_stream())
+    both = [call(stream=s) for s in streams]      # at once
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for got in both for a, b in zip(got, want))
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = call()
+    for k in range(4):                            # tokens in range, and past it again
+        d.copy_(torch.from_numpy(dh).cuda() * (0.125 if k % 2 == 0 else 1.0))
+        graph.replay()
+        torch.cuda.synchronize()
+        again = call()
+        assert all(torch.equal(a, b) for a, b in zip(out, again)), k
+        assert bool(torch.isinf(out[1]).any()) is (k % 2 == 1) and bool(torch.isfinite(out[0]).all())
